@@ -282,6 +282,126 @@ int moe_gate_bwd(const float* dw, const float* w, const int32_t* idx, const floa
                  void* dx, int dx_accumulate, void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Ragged rows (dropless layer): the chosen rows of all experts lie expert by expert in one
+ * [R, .] buffer, R = S*k, with no capacity padding between them; for a rank that holds every
+ * expert.  With n_e = min(counts[e], C):
+ *     offsets[e] = n_0 + ... + n_(e-1),   row of choice (t,j) = offsets[idx[t,j]] + slot[t,j]
+ * Choices without a slot have no row; outputs hold zeros in the rows at or behind offsets[E].  C = S
+ * drops nothing (a token asks for an expert once).
+ *
+ * moe_ragged_plan makes the rows out of what the gate wrote:
+ *   idx, slot [S, k], counts [E]  in (from moe_gate_topk with the same C)
+ *   offsets  [E+1] int32 out
+ *   row_idx, row_slot [S, k] int32 out: the row as row_idx*S + row_slot (0, -1: no row)
+ *   row_inv  [k, S] int32 out: t*k+j of the choice that has row r = S*q + s, -1 if none
+ * The R rows are thereby a buffer of k blocks of S rows, so moe_combine_fwd / moe_combine_bwd take
+ * them as they are, with E := k, C := S, idx := row_idx, slot := row_slot, inv := row_inv.
+ *
+ * The products read offsets on the device (clamped to 0..R and to rising order; no host copy is
+ * needed, calls can be captured into a graph).
+ *   x    inv != NULL: token rows [S, K], row r is token inv[r] / k (inv[r] < 0 or past the last
+ *        token: a row of zeros).  inv == NULL: rows [R, K] as they lie, k = 1, S ignored.
+ *   W    [E, K, N], or with transposed = 1 [E, N, K]
+ *   moe_ragged_gemm    Y [R, N] = X W of each row's expert; rows behind offsets[E] are zeros
+ *   moe_ragged_wgrad   dW [E, K, N] = X^T dY over the expert's rows (zeros for an expert without)
+ * fp32 accumulation in bf16, fp64 in fp32.
+ * Limits: E <= 256, K and N multiples of 8, S*k and R at most 2^29, in bf16 x, Y and one expert's
+ * matrix under 4 GiB each (MOE_EUNSUPPORTED).
+ * --------------------------------------------------------------------------------------- */
+int moe_ragged_plan(const int32_t* idx, const int32_t* slot, const int32_t* counts,
+                    int64_t S, int E, int k, int64_t C,
+                    int32_t* offsets, int32_t* row_idx, int32_t* row_slot, int32_t* row_inv,
+                    void* stream);
+
+size_t moe_ragged_gemm_workspace_bytes(int dtype, int64_t R, int E, int K, int N);
+
+int moe_ragged_gemm(const void* x, int dtype, int64_t S, const int32_t* inv, int k,
+                    const void* W, int transposed, const int32_t* offsets, int64_t R, int E, int K,
+                    int N, void* Y, void* ws, size_t ws_bytes, void* stream);
+
+size_t moe_ragged_wgrad_workspace_bytes(int dtype, int64_t R, int E, int K, int N);
+
+int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32_t* inv, int k,
+                     const void* dY, const int32_t* offsets, int64_t R, int E, int K, int N,
+                     void* dW, void* ws, size_t ws_bytes, void* stream);
+
+/* Expert FFN of one ESP shard over ragged rows (weights and shard as in moe_expert_ffn_fwd), whose
+ * pre-activation is kept for the backward pass in the 8-bit form of moe_ckpt8_store:
+ *   forward   Z = X W1[:, h0:h0+H_l], A = GeLU(Z), Y = A W2[h0:h0+H_l, :]; A and Y use Z as computed
+ *     Zq [R, H_l] int8, Zs [R, ceil(H_l/32)] uint8  out, or both NULL (nothing is kept: serving)
+ *     A  [R, H_l] scratch of the call, dtype;  Y [R, M] out, a partial sum when n_esp > 1
+ *   backward  with z the value that (Zq, Zs) stand for, in the activation as well as in its derivative:
+ *     dZ = (dY W2^T) GeLU'(z),  dX = dZ W1^T,  dW1 = X^T dZ,  dW2 = GeLU(z)^T dY
+ *     dX [R, M];  dW1, dW2 FULL tensors, only the shard's columns / rows are written
+ * The kept form takes 1 + 1/32 bytes a hidden value, where moe_expert_ffn_fwd's Z and A take 4 (bf16)
+ * or 8; the backward pass recomputes A.  Rows of Zq, Zs and A behind offsets[E] are not written.
+ * Workspace: backward, dZ and the recomputed activation. */
+size_t moe_ragged_ffn_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp,
+                                      int backward);
+
+int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int32_t* inv, int k,
+                       const void* W1, const void* W2, const int32_t* offsets, int64_t R, int E,
+                       int M, int H, int esp_idx, int n_esp, void* Zq, void* Zs, void* A, void* Y,
+                       void* ws, size_t ws_bytes, void* stream);
+
+int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int64_t S, const int32_t* inv, int k,
+                       const void* Zq, const void* Zs, const void* W1, const void* W2,
+                       const int32_t* offsets, int64_t R, int E, int M, int H, int esp_idx, int n_esp,
+                       void* dX, void* dW1, void* dW2, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits.  A row of x [rows, cols] is cut into blocks of 32 columns (the
+ * last one may be short).  With a block's largest magnitude a in [2^x, 2^(x+1)) its step is 2^(x-6),
+ * twice that where a / step would round to 128; a value is kept as the whole number nearest to
+ * value / step (ties to even), within +-127: off by at most half a step.
+ *   q [rows, cols] int8, scales [rows, ceil(cols/32)] uint8: step = 2^(scale - 133)
+ * A block with an infinity or a NaN comes back as NaN; where the doubled step would leave the range
+ * (magnitudes from 0.996 * 2^128 on) the step stays 2^121 and values saturate at 127 steps; magnitudes
+ * under 2^-126 have the step 2^-133.  cols % 8 == 0.
+ * --------------------------------------------------------------------------------------- */
+int moe_ckpt8_store(const void* x, int dtype, int64_t rows, int cols, void* q, void* scales,
+                    void* stream);
+int moe_ckpt8_load(const void* q, const void* scales, int64_t rows, int cols, void* x, int dtype,
+                   void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Norms in front of and behind a block, over rows [S, M] of `dtype`; w, b, gate, the statistics and all
+ * weight gradients are fp32, statistics and sums are formed in fp32.
+ *   MOE_NORM_LAYER  n(v) = (v - mean) / sqrt(var + eps) * w + b   (b NULL: none)
+ *   MOE_NORM_RMS    n(v) = v / sqrt(mean(v^2) + eps) * w          (b, mean and db NULL)
+ *   moe_norm_fwd            u = n(x)
+ *   moe_norm_residual_fwd   y = x + alpha * gate * n(h); gate [M] (MOE_GATE_CHANNEL), [S]
+ *                           (MOE_GATE_TOKEN) or NULL (MOE_GATE_NONE)
+ *   mean, rstd [S] out, what the backward calls read; NULL: not kept
+ * Backward:
+ *   moe_norm_residual_bwd   from dy: dh, dw, db, dgate (the gradient of x is dy itself)
+ *   moe_norm_bwd            from du: dx = dres + the gradient through n (dres NULL: the latter alone),
+ *                           dw, db
+ *   db and dgate may be NULL.  The column sums are added in a fixed order: the same bits every time.
+ * M % 8 == 0, M <= 32768.
+ * --------------------------------------------------------------------------------------- */
+enum { MOE_NORM_LAYER = 0, MOE_NORM_RMS = 1 };
+enum { MOE_GATE_NONE = 0, MOE_GATE_CHANNEL = 1, MOE_GATE_TOKEN = 2 };
+
+int moe_norm_fwd(const void* x, int dtype, int64_t S, int M, int kind, const float* w, const float* b,
+                 float eps, void* u, float* mean, float* rstd, void* stream);
+
+int moe_norm_residual_fwd(const void* h, const void* x, int dtype, int64_t S, int M, int kind,
+                          const float* w, const float* b, const float* gate, int gate_kind, float alpha,
+                          float eps, void* y, float* mean, float* rstd, void* stream);
+
+size_t moe_norm_bwd_workspace_bytes(int64_t S, int M);
+
+int moe_norm_bwd(const void* du, const void* x, int dtype, int64_t S, int M, int kind, const float* w,
+                 const float* mean, const float* rstd, const void* dres, void* dx, float* dw, float* db,
+                 void* ws, size_t ws_bytes, void* stream);
+
+int moe_norm_residual_bwd(const void* dy, const void* h, int dtype, int64_t S, int M, int kind,
+                          const float* w, const float* b, const float* gate, int gate_kind, float alpha,
+                          const float* mean, const float* rstd, void* dh, float* dw, float* db,
+                          float* dgate, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Schedule selection, Section V.  Host functions, host pointers, no GPU work.
  *
  * moe_alpha_beta_fit: least-squares fit of t = alpha + beta * x to n >= 2 measured (size, time)

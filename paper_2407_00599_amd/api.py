@@ -15,6 +15,8 @@ import torch
 
 MOE_F32, MOE_BF16 = 0, 1
 MOE_TILE_AUTO, MOE_TILE_SMALL, MOE_TILE_256, MOE_TILE_192 = 0, 1, 2, 3
+MOE_NORM_LAYER, MOE_NORM_RMS = 0, 1
+MOE_GATE_NONE, MOE_GATE_CHANNEL, MOE_GATE_TOKEN = 0, 1, 2
 MOE_GATE_STATIC_SCRATCH_BYTES = 2 << 20
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libparm_moe.so")
@@ -86,6 +88,39 @@ def lib() -> ctypes.CDLL:
         L.moe_gate_bwd.restype = c_i
         L.moe_gate_bwd.argtypes = [c_p, c_p, c_p, c_p, c_p, c_i, c_p, c_i64, c_i, c_i, c_i, c_i,
                                    c_p, c_p, c_p, c_p, c_i, c_p, c_sz, c_p]
+        c_f = ctypes.c_float
+        L.moe_ragged_plan.restype = c_i
+        L.moe_ragged_plan.argtypes = [c_p, c_p, c_p, c_i64, c_i, c_i, c_i64, c_p, c_p, c_p, c_p, c_p]
+        for f in (L.moe_ragged_gemm_workspace_bytes, L.moe_ragged_wgrad_workspace_bytes):
+            f.restype = c_sz
+            f.argtypes = [c_i, c_i64, c_i, c_i, c_i]
+        L.moe_ragged_gemm.restype = c_i
+        L.moe_ragged_gemm.argtypes = [c_p, c_i, c_i64, c_p, c_i, c_p, c_i, c_p, c_i64, c_i, c_i, c_i, c_p, c_p, c_sz, c_p]
+        L.moe_ragged_wgrad.restype = c_i
+        L.moe_ragged_wgrad.argtypes = [c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_i64, c_i, c_i, c_i, c_p, c_p, c_sz, c_p]
+        L.moe_ragged_ffn_workspace_bytes.restype = c_sz
+        L.moe_ragged_ffn_workspace_bytes.argtypes = [c_i, c_i64, c_i, c_i, c_i, c_i, c_i]
+        L.moe_ragged_ffn_fwd.restype = c_i
+        L.moe_ragged_ffn_fwd.argtypes = [c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_p, c_i64, c_i, c_i, c_i, c_i, c_i,
+                                         c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
+        L.moe_ragged_ffn_bwd.restype = c_i
+        L.moe_ragged_ffn_bwd.argtypes = [c_p, c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_i64, c_i, c_i, c_i,
+                                         c_i, c_i, c_p, c_p, c_p, c_p, c_sz, c_p]
+        L.moe_ckpt8_store.restype = c_i
+        L.moe_ckpt8_store.argtypes = [c_p, c_i, c_i64, c_i, c_p, c_p, c_p]
+        L.moe_ckpt8_load.restype = c_i
+        L.moe_ckpt8_load.argtypes = [c_p, c_p, c_i64, c_i, c_p, c_i, c_p]
+        L.moe_norm_fwd.restype = c_i
+        L.moe_norm_fwd.argtypes = [c_p, c_i, c_i64, c_i, c_i, c_p, c_p, c_f, c_p, c_p, c_p, c_p]
+        L.moe_norm_residual_fwd.restype = c_i
+        L.moe_norm_residual_fwd.argtypes = [c_p, c_p, c_i, c_i64, c_i, c_i, c_p, c_p, c_p, c_i, c_f, c_f, c_p, c_p, c_p, c_p]
+        L.moe_norm_bwd_workspace_bytes.restype = c_sz
+        L.moe_norm_bwd_workspace_bytes.argtypes = [c_i64, c_i]
+        L.moe_norm_bwd.restype = c_i
+        L.moe_norm_bwd.argtypes = [c_p, c_p, c_i, c_i64, c_i, c_i, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_p, c_sz, c_p]
+        L.moe_norm_residual_bwd.restype = c_i
+        L.moe_norm_residual_bwd.argtypes = [c_p, c_p, c_i, c_i64, c_i, c_i, c_p, c_p, c_p, c_i, c_f, c_p, c_p, c_p, c_p, c_p,
+                                            c_p, c_p, c_sz, c_p]
         _lib = L
     return _lib
 
@@ -97,6 +132,10 @@ EXPORTED = [
     "moe_expert_ffn_bwd", "moe_expert_ffn_bwd_gather",
     "moe_combine_fwd", "moe_combine_bwd", "moe_gate_bwd_workspace_bytes", "moe_gate_bwd", "moe_alpha_beta_fit",
     "moe_choose_schedule",
+    "moe_ragged_plan", "moe_ragged_gemm_workspace_bytes", "moe_ragged_gemm", "moe_ragged_wgrad_workspace_bytes",
+    "moe_ragged_wgrad", "moe_ragged_ffn_workspace_bytes", "moe_ragged_ffn_fwd", "moe_ragged_ffn_bwd",
+    "moe_ckpt8_store", "moe_ckpt8_load",
+    "moe_norm_fwd", "moe_norm_residual_fwd", "moe_norm_bwd_workspace_bytes", "moe_norm_bwd", "moe_norm_residual_bwd",
 ]
 
 
@@ -260,3 +299,108 @@ def moe_gate_bwd(dw, w, idx, logits, x, Wg, S, M, E, k, norm_topk, dlogits, dWg,
     _check((_lib or lib()).moe_gate_bwd(_ptr(dw), _ptr(w), _ptr(idx), _ptr(logits), _ptr(x), dtype_code(x), _ptr(Wg), S,
                                         M, E, k, norm_topk, _ptr(dlogits), _ptr(dWg), _ptr(dgate_bias), _ptr(dx),
                                         int(dx_accumulate), wp, wb, _stream()), "moe_gate_bwd")
+
+
+def _same_dtype(t, *others):
+    """The storage type that a call's activations and weights share."""
+    for o in others:
+        if o.dtype != t.dtype:
+            raise ValueError(f"tensors of one call differ in type: {t.dtype} and {o.dtype}")
+    return dtype_code(t)
+
+
+def _typed(dtype, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype != dtype:
+            raise ValueError(f"expected {dtype}, got {t.dtype}")
+
+
+def moe_ragged_plan(idx, slot, counts, S, E, k, C, offsets, row_idx, row_slot, row_inv):
+    _typed(torch.int32, idx, slot, counts, offsets, row_idx, row_slot, row_inv)
+    _check((_lib or lib()).moe_ragged_plan(_ptr(idx), _ptr(slot), _ptr(counts), S, E, k, C, _ptr(offsets), _ptr(row_idx),
+                                           _ptr(row_slot), _ptr(row_inv), _stream()), "moe_ragged_plan")
+
+
+def moe_ragged_gemm_workspace_bytes(dtype, R, E, K, N) -> int:
+    return int(lib().moe_ragged_gemm_workspace_bytes(dtype, R, E, K, N))
+
+
+def moe_ragged_gemm(x, S, inv, k, W, transposed, offsets, R, E, K, N, Y, ws=None):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _check((_lib or lib()).moe_ragged_gemm(_ptr(x), _same_dtype(x, W, Y), S, _ptr(inv), k, _ptr(W), transposed, _ptr(offsets),
+                                           R, E, K, N, _ptr(Y), wp, wb, _stream()), "moe_ragged_gemm")
+
+
+def moe_ragged_wgrad_workspace_bytes(dtype, R, E, K, N) -> int:
+    return int(lib().moe_ragged_wgrad_workspace_bytes(dtype, R, E, K, N))
+
+
+def moe_ragged_wgrad(x, S, inv, k, dY, offsets, R, E, K, N, dW, ws=None):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _check((_lib or lib()).moe_ragged_wgrad(_ptr(x), _same_dtype(x, dY, dW), S, _ptr(inv), k, _ptr(dY), _ptr(offsets), R, E, K,
+                                            N, _ptr(dW), wp, wb, _stream()), "moe_ragged_wgrad")
+
+
+def moe_ragged_ffn_workspace_bytes(dtype, R, E, M, H, n_esp, backward) -> int:
+    return int(lib().moe_ragged_ffn_workspace_bytes(dtype, R, E, M, H, n_esp, int(backward)))
+
+
+def moe_ragged_ffn_fwd(x, S, inv, k, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, Zq, Zs, A, Y, ws=None):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _check((_lib or lib()).moe_ragged_ffn_fwd(_ptr(x), _same_dtype(x, W1, W2, A, Y), S, _ptr(inv), k, _ptr(W1), _ptr(W2),
+                                              _ptr(offsets), R, E, M, H, esp_idx, n_esp, _ptr(Zq), _ptr(Zs), _ptr(A),
+                                              _ptr(Y), wp, wb, _stream()), "moe_ragged_ffn_fwd")
+
+
+def moe_ragged_ffn_bwd(dY, x, S, inv, k, Zq, Zs, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, dX, dW1, dW2, ws):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _check((_lib or lib()).moe_ragged_ffn_bwd(_ptr(dY), _ptr(x), _same_dtype(x, dY, W1, W2, dX, dW1, dW2), S, _ptr(inv), k,
+                                              _ptr(Zq), _ptr(Zs), _ptr(W1), _ptr(W2), _ptr(offsets), R, E, M, H, esp_idx,
+                                              n_esp, _ptr(dX), _ptr(dW1), _ptr(dW2), wp, wb, _stream()), "moe_ragged_ffn_bwd")
+
+
+def moe_ckpt8_store(x, rows, cols, q, scales):
+    _check((_lib or lib()).moe_ckpt8_store(_ptr(x), dtype_code(x), rows, cols, _ptr(q), _ptr(scales), _stream()),
+           "moe_ckpt8_store")
+
+
+def moe_ckpt8_load(q, scales, rows, cols, x):
+    _check((_lib or lib()).moe_ckpt8_load(_ptr(q), _ptr(scales), rows, cols, _ptr(x), dtype_code(x), _stream()),
+           "moe_ckpt8_load")
+
+
+def moe_norm_fwd(x, S, M, kind, w, b, eps, u, mean=None, rstd=None):
+    _typed(torch.float32, w, b, mean, rstd)
+    _check((_lib or lib()).moe_norm_fwd(_ptr(x), _same_dtype(x, u), S, M, kind, _ptr(w), _ptr(b), eps, _ptr(u), _ptr(mean),
+                                        _ptr(rstd), _stream()), "moe_norm_fwd")
+
+
+def moe_norm_residual_fwd(h, x, S, M, kind, w, b, gate, gate_kind, alpha, eps, y, mean=None, rstd=None):
+    _typed(torch.float32, w, b, gate, mean, rstd)
+    _check((_lib or lib()).moe_norm_residual_fwd(_ptr(h), _ptr(x), _same_dtype(h, x, y), S, M, kind, _ptr(w), _ptr(b),
+                                                 _ptr(gate), gate_kind, alpha, eps, _ptr(y), _ptr(mean), _ptr(rstd),
+                                                 _stream()), "moe_norm_residual_fwd")
+
+
+def moe_norm_bwd_workspace_bytes(S, M) -> int:
+    return int(lib().moe_norm_bwd_workspace_bytes(S, M))
+
+
+def moe_norm_bwd(du, x, S, M, kind, w, mean, rstd, dres, dx, dw, db, ws):
+    wp, wb = _ws_args(ws)
+    _typed(torch.float32, w, mean, rstd, dw, db)
+    _check((_lib or lib()).moe_norm_bwd(_ptr(du), _ptr(x), _same_dtype(x, du, dx), S, M, kind, _ptr(w), _ptr(mean),
+                                        _ptr(rstd), _ptr(dres), _ptr(dx), _ptr(dw), _ptr(db), wp, wb, _stream()),
+           "moe_norm_bwd")
+
+
+def moe_norm_residual_bwd(dy, h, S, M, kind, w, b, gate, gate_kind, alpha, mean, rstd, dh, dw, db, dgate, ws):
+    wp, wb = _ws_args(ws)
+    _typed(torch.float32, w, b, gate, mean, rstd, dw, db, dgate)
+    _check((_lib or lib()).moe_norm_residual_bwd(_ptr(dy), _ptr(h), _same_dtype(h, dy, dh), S, M, kind, _ptr(w), _ptr(b),
+                                                 _ptr(gate), gate_kind, alpha, _ptr(mean), _ptr(rstd), _ptr(dh), _ptr(dw),
+                                                 _ptr(db), _ptr(dgate), wp, wb, _stream()), "moe_norm_residual_bwd")

@@ -15,7 +15,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libparm_moe.so")
-SOURCES = ["api.hip", "gate.hip", "permute.hip", "ffn.hip", "gate_bwd.hip", "schedule.hip"]
+SOURCES = ["api.hip", "gate.hip", "permute.hip", "ffn.hip", "gate_bwd.hip", "schedule.hip", "ragged.hip",
+           "ckpt8.hip", "norm.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-fvisibility=default",
@@ -27,7 +28,7 @@ FLAGS = [
 # front of them moves them: the merged backward launch of 8 experts x 16384 x 4096 x 7168, same loops, 17.44 ms with a loop at
 # the start of a line and 17.78 behind it; the call 21.96 / 22.19 / 21.90 ms (by chance aligned / moved / aligned by this).  The
 # padding costs where short loops nest (slots of the gate 6.4 -> 6.6 us), so the other sources go without.
-FILE_FLAGS = {"ffn.hip": ["-Xarch_device", "-falign-loops=64"]}
+FILE_FLAGS = {f: ["-Xarch_device", "-falign-loops=64"] for f in ("ffn.hip", "ragged.hip")}
 
 
 def _stale() -> bool:
