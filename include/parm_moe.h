@@ -304,7 +304,7 @@ int moe_gate_bwd(const float* dw, const float* w, const int32_t* idx, const floa
  *   W    [E, K, N], or with transposed = 1 [E, N, K]
  *   moe_ragged_gemm    Y [R, N] = X W of each row's expert; rows behind offsets[E] are zeros
  *   moe_ragged_wgrad   dW [E, K, N] = X^T dY over the expert's rows (zeros for an expert without)
- * fp32 accumulation in bf16, fp64 in fp32.
+ * fp32 accumulation.
  * Limits: E <= 256, K and N multiples of 8, S*k and R at most 2^29, in bf16 x, Y and one expert's
  * matrix under 4 GiB each (MOE_EUNSUPPORTED).
  * --------------------------------------------------------------------------------------- */
@@ -328,7 +328,9 @@ int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32_t* inv, in
 /* Expert FFN of one ESP shard over ragged rows (weights and shard as in moe_expert_ffn_fwd), whose
  * pre-activation is kept for the backward pass in the 8-bit form of moe_ckpt8_store:
  *   forward   Z = X W1[:, h0:h0+H_l], A = GeLU(Z), Y = A W2[h0:h0+H_l, :]; A and Y use Z as computed
- *     Zq [R, H_l] int8, Zs [R, ceil(H_l/32)] uint8  out, or both NULL (nothing is kept: serving)
+ *     Zq [R, H_l] int8, Zs [R, ceil(H_l/32)] uint8  out, or both NULL (nothing is kept: serving);
+ *     from fp32 operands a kept Z is accumulated in fp64, because a sum next to the border between two
+ *     steps decides which one is kept
  *     A  [R, H_l] scratch of the call, dtype;  Y [R, M] out, a partial sum when n_esp > 1
  *   backward  with z the value that (Zq, Zs) stand for, in the activation as well as in its derivative:
  *     dZ = (dY W2^T) GeLU'(z),  dX = dZ W1^T,  dW1 = X^T dZ,  dW2 = GeLU(z)^T dY

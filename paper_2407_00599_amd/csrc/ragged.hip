@@ -13,7 +13,7 @@
 #include <math.h>
 
 #include "ckpt8.h"
-#include "ffn_tile.h"
+#include "ragged.h"
 
 namespace moe {
 
@@ -61,112 +61,12 @@ __global__ __launch_bounds__(PLAN_THREADS) void ragged_plan(const int32_t* __res
 // ------------------------------------------------------------------------------------------
 // layout of the tiles
 // ------------------------------------------------------------------------------------------
-enum { EPI_ACT = 16, EPI_GELU8 = 17, EPI_DGELU8 = 18 };   // GeLU alone; GeLU and the 8-bit form; dZ and GeLU from the 8-bit form
-
-struct RaggedArgs : GemmArgs {     // G = E experts, Cc = R = rows of the buffers, Mdim = R in row-tiled GEMMs, C2 / Zin = the 8-bit values
-  const int32_t* off;              // [E + 1]
-  uint8_t* Zs;                     // [R, ldz] scales of the 8-bit values
-  int ldz;
-  int grid;                        // workgroups of this problem
-};
-
-// GeLU(z) = z Phi(z) and GeLU'(z) = Phi(z) + z phi(z).  Phi(z) - 1/2 is the odd minimax polynomial of fit_gelu_poly.py on |z| <= 4.25
-// (absolute error 1.2e-5), clamped outside; phi is exp2 of the hardware.
-__device__ constexpr float PHI_ODD[9] = {3.989023268e-01f, -6.634449214e-02f, 9.815968573e-03f, -1.108560129e-03f,
-                                         9.341852274e-05f, -5.626405255e-06f, 2.255412426e-07f, -5.327701835e-09f,
-                                         5.564777111e-11f};
-__device__ __forceinline__ float normal_cdf(float z) {
-  const float zc = __builtin_amdgcn_fmed3f(z, -4.25f, 4.25f), u = zc * zc;
-  float q = fmaf(PHI_ODD[8], u, PHI_ODD[7]);
-#pragma unroll
-  for (int i = 6; i >= 0; --i) q = fmaf(q, u, PHI_ODD[i]);
-  return __builtin_amdgcn_fmed3f(fmaf(zc, q, 0.5f), 0.0f, 1.0f);
-}
-__device__ __forceinline__ float gelu_fast(float z) { return z * normal_cdf(z); }
-__device__ __forceinline__ void gelu_and_grad_fast(float z, float& g, float& dg) {
-  const float cdf = normal_cdf(z);
-  g = z * cdf;
-  dg = fmaf(z * 0.39894228040143267794f, __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f), cdf);   // (1/2) log2(e)
-}
-
 struct Ragged {
   using Args = RaggedArgs;
-  struct Place {
-    int g, tm, tn;
-    int lo, n;        // first row and number of rows of expert g
-  };
-  static __device__ __forceinline__ int offset(const Args& p, int e) { return min(max(p.off[e], 0), p.R); }
+  using Place = RaggedPlace;
 
-  // Tiles of a row-tiled GEMM in linear order expert by expert, each with ceil(n / TM) row tiles; XCDs and patches as in the padded
-  // calls.  The grid is made for the most tiles that R rows can have, and the workgroups behind the last tile store the rows
-  // behind offsets[E] as zeros, an equal share each.
   template <int KIND, int EPI, int ESZ, int TM, int TN>
-  static __device__ __forceinline__ bool find(const Args& p, int vb, Place& at) {
-    const int x = vb & 7, i = vb >> 3, lane = threadIdx.x & 63;
-    if (KIND == KIND_TN) {
-      const int per_xcd = (p.total_tiles + 7) / 8, tile = xcd_tile(p, x, i, per_xcd), per_g = p.tiles_m * p.tiles_n;
-      if (i >= per_xcd || tile >= p.total_tiles) return false;
-      at.g = tile / per_g;
-      patch_order(tile - at.g * per_g, p.tiles_m, p.tiles_n, at.tm, at.tn);
-      at.lo = __builtin_amdgcn_readfirstlane(offset(p, at.g));
-      at.n = __builtin_amdgcn_readfirstlane(max(offset(p, at.g + 1) - at.lo, 0));
-      return true;
-    }
-    // 64 experts at a time, a lane each
-    int lo = 0, n = 0, m = 0, incl = 0;
-    auto scan = [&](int e0) {
-      const int e = e0 + lane;
-      lo = offset(p, min(e, p.G));
-      n = e < p.G ? max(offset(p, min(e + 1, p.G)) - lo, 0) : 0;
-      m = (n + TM - 1) / TM;
-      incl = m;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(incl, d, 64);
-        if (lane >= d) incl += v;
-      }
-      return __builtin_amdgcn_readlane(incl, 63);
-    };
-    int all = 0;
-    for (int e0 = 0; e0 < p.G; e0 += 64) all += scan(e0);
-    const int T = all * p.tiles_n, per_t = (T + 7) / 8;
-    if (i >= per_t) {
-      if (EPI == EPI_STORE) fill_behind<ESZ>(p, (i - per_t) * 8 + x, p.grid - 8 * per_t);
-      return false;
-    }
-    const int tile = xcd_tile(p, x, i, per_t);
-    if (tile >= T) return false;
-    int run = 0;
-    for (int e0 = 0; e0 < p.G; e0 += 64) {
-      if (p.G > 64) scan(e0);
-      const unsigned long long hit = __ballot((run + incl) * p.tiles_n > tile);
-      if (hit) {
-        const int l = __ffsll((long long)hit) - 1;
-        at.g = e0 + l;
-        at.lo = __builtin_amdgcn_readlane(lo, l);
-        at.n = __builtin_amdgcn_readlane(n, l);
-        patch_order(tile - (run + __builtin_amdgcn_readlane(incl - m, l)) * p.tiles_n, __builtin_amdgcn_readlane(m, l), p.tiles_n,
-                    at.tm, at.tn);
-        return true;
-      }
-      run += __builtin_amdgcn_readlane(incl, 63);
-    }
-    return false;
-  }
-  // share `at` of `shares` of the rows behind the last expert's
-  template <int ESZ>
-  static __device__ __forceinline__ void fill_behind(const Args& p, int at, int shares) {
-    const int64_t row_units = p.ldc * ESZ / 16, r0 = offset(p, p.G), units = (p.R - r0) * row_units;
-    if (units <= 0 || at >= shares) return;
-    const int64_t per = (units + shares - 1) / shares, u1 = min(per * (at + 1), units);
-    u32x4_t* c = reinterpret_cast<u32x4_t*>(p.C) + r0 * row_units;
-    const u32x4_t z = {0u, 0u, 0u, 0u};
-    for (int64_t u = per * at + threadIdx.x; u < u1; u += blockDim.x) __builtin_nontemporal_store(z, c + u);
-  }
-  static __device__ __forceinline__ int token(const Args& p, int iv) {   // -1: no token, a row of zeros
-    const uint32_t tok = p.gather_k == 1 ? (uint32_t)iv : __umulhi((uint32_t)iv, p.gather_magic);
-    return iv >= 0 && (int64_t)tok < p.gather_rows ? (int)tok : -1;
-  }
+  static __device__ __forceinline__ bool find(const Args& p, int vb, Place& at) { return find_tile<KIND, EPI, ESZ, TM, TN>(p, vb, at); }
   template <int TM, int RA>
   static __device__ __forceinline__ void rows(const Args& p, const Place& at, int q0, int w0, int (&q_row)[RA], uint32_t (&out_off)[2]) {
     int r[RA + 2], row[RA + 2];
@@ -400,74 +300,39 @@ struct Ragged {
                                                    int rw, int kw, int lane, int o_row, bool o_zero) {
     constexpr int NJ = TN / 16;
     float* __restrict__ C = reinterpret_cast<float*>(p.C);
-    if constexpr (EPI == EPI_GELU8) {
-      constexpr int PITCH = TN + 1, UNITS = TM * TN / 32, TPU = 256 / UNITS, CPT = 32 / TPU;   // blocks; threads and columns of each
-      static_assert(TM * PITCH * 8 <= f32_lds<TM, TN>() && CPT % 4 == 0, "the tile fits in the buffers");
-      __syncthreads();
+    constexpr int PITCH = TN + 1, UNITS = TM * TN / 32, TPU = 256 / UNITS, CPT = 32 / TPU;   // blocks; threads and columns of each
+    static_assert(EPI == EPI_GELU8, "the other products are on the fp32 matrix cores");
+    static_assert(TM * PITCH * 8 <= f32_lds<TM, TN>() && CPT % 4 == 0, "the tile fits in the buffers");
+    __syncthreads();
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int j = 0; j < NJ / KW; ++j) Bs[(rw * 16 + 4 * r + (lane >> 4)) * PITCH + 16 * (KW * j + kw) + (lane & 15)] = acc[j][r];
-      __syncthreads();
-      const int tid = threadIdx.x, unit = tid / TPU, ml = unit / (TN / 32), c0 = unit % (TN / 32) * 32 + tid % TPU * CPT;
-      const int row = __shfl(o_row, ml & 63, 64), n = n0 + c0;
-      const bool zero = __shfl((int)o_zero, ml & 63, 64) != 0;
-      double z[CPT];
-      uint32_t top = 0;
+      for (int j = 0; j < NJ / KW; ++j) Bs[(rw * 16 + 4 * r + (lane >> 4)) * PITCH + 16 * (KW * j + kw) + (lane & 15)] = acc[j][r];
+    __syncthreads();
+    const int tid = threadIdx.x, unit = tid / TPU, ml = unit / (TN / 32), c0 = unit % (TN / 32) * 32 + tid % TPU * CPT;
+    const int row = __shfl(o_row, ml & 63, 64), n = n0 + c0;
+    const bool zero = __shfl((int)o_zero, ml & 63, 64) != 0;
+    double z[CPT];
+    uint32_t top = 0;
 #pragma unroll
-      for (int u = 0; u < CPT; ++u) {
-        z[u] = zero || n + u >= p.Ndim ? 0.0 : Bs[ml * PITCH + c0 + u];
-        top = max(top, __float_as_uint((float)z[u]) & 0x7FFFFFFFu);
-      }
-#pragma unroll
-      for (int d = 1; d < TPU; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-      const int b = ckpt8_scale(top);
-      if (row < 0) return;
-#pragma unroll
-      for (int u = 0; u < CPT; u += 4) {
-        if (n + u >= p.Ndim) break;
-        float4 a;
-        a.x = gelu_f((float)z[u]); a.y = gelu_f((float)z[u + 1]); a.z = gelu_f((float)z[u + 2]); a.w = gelu_f((float)z[u + 3]);
-        *reinterpret_cast<float4*>(C + (int64_t)row * p.ldc + n + u) = a;
-        const double q[4] = {z[u], z[u + 1], z[u + 2], z[u + 3]};
-        *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(p.C2) + (int64_t)row * p.ldc + n + u) = ckpt8_pack(q, b);
-      }
-      if (tid % TPU == 0 && n < p.Ndim) p.Zs[(int64_t)row * p.ldz + (n >> 5)] = (uint8_t)b;
-      return;
+    for (int u = 0; u < CPT; ++u) {
+      z[u] = zero || n + u >= p.Ndim ? 0.0 : Bs[ml * PITCH + c0 + u];
+      top = max(top, __float_as_uint((float)z[u]) & 0x7FFFFFFFu);
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int ml = rw * 16 + 4 * r + (lane >> 4);
-      int64_t crow;
-      int row = 0;
-      bool zero = false;
-      if (KIND == KIND_TN) {
-        if (m0 + ml >= p.Mdim) continue;
-        crow = (int64_t)g * p.c_goff + p.c_off + (int64_t)(m0 + ml) * p.ldc;
-      } else {
-        row = __shfl(o_row, ml, 64);
-        zero = __shfl((int)o_zero, ml, 64) != 0;
-        if (row < 0) continue;
-        crow = (int64_t)row * p.ldc;
-      }
+    for (int d = 1; d < TPU; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
+    const int b = ckpt8_scale(top);
+    if (row < 0) return;
 #pragma unroll
-      for (int j = 0; j < NJ / KW; ++j) {
-        const int n = n0 + 16 * (KW * j + kw) + (lane & 15);
-        if (n >= p.Ndim) continue;
-        const float v = zero ? 0.f : (float)acc[j][r];
-        if (EPI == EPI_STORE) {
-          C[crow + n] = v;
-        } else if (EPI == EPI_ACT) {
-          C[crow + n] = gelu_f(v);
-        } else {
-          float ge, dg;
-          const uint32_t q = reinterpret_cast<const uint8_t*>(p.Zin)[crow + n];
-          gelu_and_grad(ckpt8_value(q, 0, p.Zs[(int64_t)row * p.ldz + (n >> 5)]), ge, dg);
-          C[crow + n] = v * dg;
-          reinterpret_cast<float*>(p.C2)[crow + n] = ge;
-        }
-      }
+    for (int u = 0; u < CPT; u += 4) {
+      if (n + u >= p.Ndim) break;
+      float4 a;
+      a.x = gelu_f((float)z[u]); a.y = gelu_f((float)z[u + 1]); a.z = gelu_f((float)z[u + 2]); a.w = gelu_f((float)z[u + 3]);
+      *reinterpret_cast<float4*>(C + (int64_t)row * p.ldc + n + u) = a;
+      const double q[4] = {z[u], z[u + 1], z[u + 2], z[u + 3]};
+      *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(p.C2) + (int64_t)row * p.ldc + n + u) = ckpt8_pack(q, b);
     }
+    if (tid % TPU == 0 && n < p.Ndim) p.Zs[(int64_t)row * p.ldz + (n >> 5)] = (uint8_t)b;
   }
 };
 
@@ -477,10 +342,40 @@ __global__ __launch_bounds__(64 * CF::NW) void ragged_ffn_gemm_dma(const RaggedA
   gemm_dma_tile<KIND, EPI, CF, ROWS, Ragged>(p, smem, (int)blockIdx.x);
 }
 
-template <int KIND, int EPI, int T, bool WIDE>   // T x T tiles
-__global__ __launch_bounds__(256, 4) void ragged_ffn_gemm_f32(const RaggedArgs p) {
+// The pre-activation that is kept: on the fp64 matrix cores, because a sum next to the border between two steps decides which one is kept.
+template <int T, bool WIDE>   // T x T tiles
+__global__ __launch_bounds__(256, 4) void ragged_kept_f32(const RaggedArgs p) {
   __shared__ __attribute__((aligned(16))) double smem[f32_lds<T, T>() / 8];
-  gemm_f32_tile<KIND, EPI, T, T, WIDE, Ragged>(p, smem, (int)blockIdx.x);
+  gemm_f32_tile<KIND_NN, EPI_GELU8, T, T, WIDE, Ragged>(p, smem, (int)blockIdx.x);
+}
+
+// dX = dZ W1^T and the two weight gradients, which only depend on dZ, in one launch; the third problem gathers its rows
+template <typename CFX, typename CFW, int EPI>
+__global__ __launch_bounds__(512) void ragged_ffn_bwd_trio(const RaggedArgs px, const RaggedArgs pw2, const RaggedArgs pw1, int nbx, int nb2) {
+  static_assert(CFX::NW == 8 && CFW::NW == 8, "one block size");
+  __shared__ __attribute__((aligned(1024))) char smem[CFX::LDS > CFW::LDS ? CFX::LDS : CFW::LDS];
+  const int b = (int)blockIdx.x;
+  if (b < nbx) gemm_dma_tile<KIND_NT, EPI_STORE, CFX, ROWS_PLAIN, Ragged>(px, smem, b);
+  else if (b < nbx + nb2) gemm_dma_tile<KIND_TN, EPI, CFW, ROWS_PLAIN, Ragged>(pw2, smem, b - nbx);
+  else gemm_dma_tile<KIND_TN, EPI, CFW, ROWS_GATHER, Ragged>(pw1, smem, b - nbx - nb2);
+}
+
+// Adds the parts of one or two split weight gradients in order and stores them: a thread owns 4 columns of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void ragged_add_parts(const RaggedArgs p2, const RaggedArgs p1, int64_t n2, int64_t n) {
+  int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (u >= n) return;
+  const RaggedArgs& p = u < n2 ? p2 : p1;
+  if (u >= n2) u -= n2;
+  const int64_t size = (int64_t)p.G * p.Mdim * p.Ndim, at = u * 4;
+  const float* src = p.part + at;
+  f32x4_t v = *reinterpret_cast<const f32x4_t*>(src);
+#pragma unroll 8
+  for (int q = 1; q < p.splits; ++q) v += *reinterpret_cast<const f32x4_t*>(src + q * size);
+  const int64_t row = at / p.Ndim, g = row / p.Mdim;
+  T* dst = reinterpret_cast<T*>(p.C) + g * p.c_goff + p.c_off + (row - g * p.Mdim) * p.ldc + (at - row * p.Ndim);
+  if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+  else *reinterpret_cast<f32x4_t*>(dst) = v;
 }
 
 // ------------------------------------------------------------------------------------------
@@ -488,23 +383,17 @@ __global__ __launch_bounds__(256, 4) void ragged_ffn_gemm_f32(const RaggedArgs p
 // ------------------------------------------------------------------------------------------
 namespace {
 
-// Row tiles that R rows of E experts are priced at: half a tile of each expert's last one is empty.  How the rows are spread is not
-// known here.
-double priced_row_tiles(int R, int E, int tile_m) {
-  const double rows = (double)R / E;
-  return E * (rows < 1.0 ? rows : std::max(1.0, rows / tile_m + 0.45));
-}
-// the most row tiles that R rows of E experts can have
-int64_t most_row_tiles(int R, int E, int tile_m) {
-  const int64_t used = std::min(R, E);
-  return ((int64_t)R + used * (tile_m - 1)) / tile_m;
+void buffer_sizes(RaggedArgs& a, bool weights) {
+  a.a_bytes = (a.gather ? (uint64_t)a.gather_rows : (uint64_t)a.R) * (uint64_t)a.lda * 2;
+  a.b_bytes = weights ? (uint64_t)a.R * (uint64_t)a.ldb * 2 : (uint64_t)a.G * (uint64_t)a.b_goff * 2;
 }
 
-TilePlan plan_rows(const RaggedArgs& a) {
+TilePlan plan_rows(const RaggedArgs& a, bool wide = false) {   // wide: only tiles of eight waves
   const float nk = (float)((a.Kdim + DK - 1) / DK), cu = (float)num_cus();
   TilePlan best{256, 256};
   float best_t = 0.f;
   for (const TileCost& c : ROW_TILES) {
+    if (wide && c.tile.tile_n == 64) continue;
     const float n = (float)(priced_row_tiles(a.R, a.G, c.tile.tile_m) * ((a.Ndim + c.tile.tile_n - 1) / c.tile.tile_n));
     const float busy = c.per_cu == 1 ? n / cu : (n - cu) / cu;
     const float k = c.k_few + (c.k_all - c.k_few) * fminf(fmaxf(busy, 0.f), 1.f);
@@ -514,36 +403,29 @@ TilePlan plan_rows(const RaggedArgs& a) {
   return best;
 }
 
-constexpr int ZERO_SHARES = 64;    // workgroups at least that can store rows behind the last expert's
+void launch_kept_f32(RaggedArgs a, hipStream_t st) {
+  auto launch = [&](auto tile, auto wide) {
+    constexpr int T = decltype(tile)::value;
+    const dim3 grid = size_rows(a, T, T, false);
+    hipLaunchKernelGGL((ragged_kept_f32<T, decltype(wide)::value>), grid, dim3(256), 0, st, a);
+  };
+  using std::integral_constant;
+  if (std::max(a.lda, a.ldb) >= 1 << 24) launch(integral_constant<int, 32>{}, std::true_type{});
+  else if (priced_row_tiles(a.R, a.G, 64) * ((a.Ndim + 63) / 64) >= 3.0 * num_cus()) launch(integral_constant<int, 64>{}, std::false_type{});
+  else launch(integral_constant<int, 32>{}, std::false_type{});
+}
+
 template <int KIND, int EPI>
 void launch_rows(RaggedArgs a, int dtype, hipStream_t st) {
-  auto sizes = [&](int tile_m, int tile_n) {
-    const int64_t row_tiles = most_row_tiles(a.R, a.G, tile_m);
-    a.tiles_m = (int)row_tiles;
-    a.tiles_n = (a.Ndim + tile_n - 1) / tile_n;
-    a.total_tiles = (int)(row_tiles * a.tiles_n);
-    a.grid = (a.total_tiles + 7) / 8 * 8 + (EPI == EPI_STORE ? ZERO_SHARES : 0);
-    a.run_mask = ~31;
-    return dim3((unsigned)a.grid);
-  };
   if (dtype == MOE_F32) {
-    auto launch = [&](auto tile, auto wide) {
-      constexpr int T = decltype(tile)::value;
-      const dim3 grid = sizes(T, T);
-      hipLaunchKernelGGL((ragged_ffn_gemm_f32<KIND, EPI, T, decltype(wide)::value>), grid, dim3(256), 0, st, a);
-    };
-    const bool wide = std::max(a.lda, a.ldb) >= 1 << 24;
-    const double tiles64 = priced_row_tiles(a.R, a.G, 64) * ((a.Ndim + 63) / 64);
-    if (wide) launch(std::integral_constant<int, 32>{}, std::true_type{});
-    else if (tiles64 >= 3.0 * num_cus()) launch(std::integral_constant<int, 64>{}, std::false_type{});
-    else launch(std::integral_constant<int, 32>{}, std::false_type{});
+    if constexpr (EPI == EPI_GELU8) launch_kept_f32(a, st);
+    else launch_f32<KIND, EPI>(a, st);
     return;
   }
-  a.a_bytes = (a.gather ? (uint64_t)a.gather_rows : (uint64_t)a.R) * (uint64_t)a.lda * 2;
-  a.b_bytes = (uint64_t)a.G * (uint64_t)a.b_goff * 2;
+  buffer_sizes(a, false);
   auto launch = [&](auto cfg) {
     using CF = decltype(cfg);
-    const dim3 grid = sizes(CF::TM, CF::TN);
+    const dim3 grid = size_rows(a, CF::TM, CF::TN, EPI == EPI_STORE);
     hipLaunchKernelGGL((ragged_ffn_gemm_dma<KIND, EPI, CF>), grid, dim3(64 * CF::NW), 0, st, a);
   };
   const TilePlan t = plan_rows(a);
@@ -555,39 +437,85 @@ void launch_rows(RaggedArgs a, int dtype, hipStream_t st) {
   else launch(Tile32x64{});
 }
 
-void launch_weights(RaggedArgs a, int dtype, hipStream_t st) {
-  auto sizes = [&](int tile) {
-    a.tiles_m = (a.Mdim + tile - 1) / tile;
-    a.tiles_n = (a.Ndim + tile - 1) / tile;
-    a.total_tiles = a.G * a.tiles_m * a.tiles_n;
-    a.run_mask = ~31;
-    a.grid = (a.total_tiles + 7) / 8 * 8;
-    return dim3((unsigned)a.grid);
-  };
+// Weight gradients.  Tiles of 128 x 128 where those of 256 x 256 would be fewer than 64; of fp32, 64 x 64.  With few tiles a reduction over
+// thousands of rows is what a launch waits for: it is cut into parts of at least PART_TILES k tiles of an expert's mean share of the
+// rows, as many as the chip has room for (two workgroups of 128 x 128, four of fp32, to a compute unit).  Arithmetic on the shape: the parts
+// are a part of the workspace's size.
+constexpr int CHIP_CUS = 256;   // compute units of an MI355X
+constexpr int PART_TILES = 12;
+bool small_weights(int E, int M, int N) { return (int64_t)E * ((M + 255) / 256) * ((N + 255) / 256) < 64; }
+int weight_parts(int dtype, int64_t R, int E, int M, int N, int problems) {
+  if (dtype == MOE_BF16 && !small_weights(E, M, N)) return 1;
+  const int tile = dtype == MOE_BF16 ? 128 : F32_TILE, room = (dtype == MOE_BF16 ? 2 : 4) * CHIP_CUS;
+  const int64_t tiles = (int64_t)problems * E * ((M + tile - 1) / tile) * ((N + tile - 1) / tile), nk = R / E / DK;
+  const int64_t parts = std::min<int64_t>({room / tiles, nk / PART_TILES, 64});
+  return parts < 2 ? 1 : (int)parts;
+}
+size_t part_bytes(int parts, int E, int M, int N) { return parts > 1 ? align_up((size_t)parts * E * M * N * 4, 256) : 0; }
+
+void add_parts(const RaggedArgs& p2, const RaggedArgs& p1, int problems, int dtype, hipStream_t st) {
+  const int64_t n = (int64_t)p2.G * p2.Mdim * p2.Ndim / 4;       // sizes are multiples of 8
+  const dim3 grid((unsigned)((problems * n + 255) / 256));
+  if (dtype == MOE_BF16) hipLaunchKernelGGL((ragged_add_parts<bf16_t>), grid, dim3(256), 0, st, p2, p1, n, problems * n);
+  else hipLaunchKernelGGL((ragged_add_parts<float>), grid, dim3(256), 0, st, p2, p1, n, problems * n);
+}
+
+// one weight gradient; parts: room for a.splits of them
+void launch_weights(RaggedArgs a, int dtype, float* parts, hipStream_t st) {
+  a.part = parts;
   if (dtype == MOE_F32) {
-    const bool wide = std::max(a.lda, a.ldb) >= 1 << 24;
-    const int64_t tiles64 = (int64_t)a.G * ((a.Mdim + 63) / 64) * ((a.Ndim + 63) / 64);
-    auto launch = [&](auto tile, auto w) {
-      constexpr int T = decltype(tile)::value;
-      const dim3 grid = sizes(T);
-      hipLaunchKernelGGL((ragged_ffn_gemm_f32<KIND_TN, EPI_STORE, T, decltype(w)::value>), grid, dim3(256), 0, st, a);
+    if (a.splits > 1) launch_f32<KIND_TN, EPI_PART>(a, st);
+    else launch_f32<KIND_TN, EPI_STORE>(a, st);
+  } else {
+    buffer_sizes(a, true);
+    auto launch = [&](auto cfg, auto epi) {
+      using CF = decltype(cfg);
+      constexpr int EPI = decltype(epi)::value;
+      const dim3 grid(size_weights(a, CF::TM).x * a.splits);
+      if (a.gather) hipLaunchKernelGGL((ragged_ffn_gemm_dma<KIND_TN, EPI, CF, ROWS_GATHER>), grid, dim3(64 * CF::NW), 0, st, a);
+      else hipLaunchKernelGGL((ragged_ffn_gemm_dma<KIND_TN, EPI, CF>), grid, dim3(64 * CF::NW), 0, st, a);
     };
-    if (wide) launch(std::integral_constant<int, 32>{}, std::true_type{});
-    else if (tiles64 >= 3 * (int64_t)num_cus()) launch(std::integral_constant<int, 64>{}, std::false_type{});
-    else launch(std::integral_constant<int, 32>{}, std::false_type{});
-    return;
+    using Store = std::integral_constant<int, EPI_STORE>;
+    if (!small_weights(a.G, a.Mdim, a.Ndim)) launch(Tile256{}, Store{});
+    else if (a.splits > 1) launch(Tile128{}, std::integral_constant<int, EPI_PART>{});
+    else launch(Tile128{}, Store{});
   }
-  a.a_bytes = (a.gather ? (uint64_t)a.gather_rows : (uint64_t)a.R) * (uint64_t)a.lda * 2;
-  a.b_bytes = (uint64_t)a.R * (uint64_t)a.ldb * 2;
-  auto launch = [&](auto cfg) {
-    using CF = decltype(cfg);
-    const dim3 grid = sizes(CF::TM);
-    if (a.gather) hipLaunchKernelGGL((ragged_ffn_gemm_dma<KIND_TN, EPI_STORE, CF, ROWS_GATHER>), grid, dim3(64 * CF::NW), 0, st, a);
-    else hipLaunchKernelGGL((ragged_ffn_gemm_dma<KIND_TN, EPI_STORE, CF>), grid, dim3(64 * CF::NW), 0, st, a);
-  };
-  const int64_t tiles256 = (int64_t)a.G * ((a.Mdim + 255) / 256) * ((a.Ndim + 255) / 256);
-  if (tiles256 >= 64) launch(Tile256{});
-  else launch(Tile128{});
+  if (a.splits > 1) add_parts(a, a, 1, dtype, st);
+}
+
+// dX and the two weight gradients of the FFN
+void launch_backward(RaggedArgs dx, RaggedArgs w2, RaggedArgs w1, int dtype, float* parts, hipStream_t st) {
+  w2.part = parts;
+  w1.part = w2.splits > 1 ? parts + (size_t)w2.splits * w2.G * w2.Mdim * w2.Ndim : nullptr;
+  if (dtype == MOE_F32) {
+    launch_trio_f32(dx, w2, w1, st);
+  } else if (w1.gather == nullptr) {
+    launch_rows<KIND_NT, EPI_STORE>(dx, dtype, st);
+    launch_weights(w2, dtype, w2.part, st);
+    launch_weights(w1, dtype, w1.part, st);
+    return;
+  } else {
+    buffer_sizes(dx, false); buffer_sizes(w2, true); buffer_sizes(w1, true);
+    auto launch = [&](auto cfx, auto cfw, auto epi) {
+      using CFX = decltype(cfx);
+      using CFW = decltype(cfw);
+      const unsigned nbx = size_rows(dx, CFX::TM, CFX::TN, true).x;
+      const unsigned nb2 = size_weights(w2, CFW::TM).x * w2.splits, nb1 = size_weights(w1, CFW::TM).x * w1.splits;
+      hipLaunchKernelGGL((ragged_ffn_bwd_trio<CFX, CFW, decltype(epi)::value>), dim3(nbx + nb2 + nb1), dim3(512), 0, st, dx, w2, w1, (int)nbx, (int)nb2);
+    };
+    using Store = std::integral_constant<int, EPI_STORE>;
+    if (small_weights(w2.G, w2.Mdim, w2.Ndim)) {
+      if (w2.splits > 1) launch(Tile64x128{}, Tile128{}, std::integral_constant<int, EPI_PART>{});
+      else launch(Tile64x128{}, Tile128{}, Store{});
+    } else {
+      const TilePlan t = plan_rows(dx, true);
+      if (t.tile_m == 256) launch(Tile256{}, Tile256{}, Store{});
+      else if (t.tile_m == 192) launch(Tile192{}, Tile256{}, Store{});
+      else if (t.tile_m == 128) launch(Tile128{}, Tile256{}, Store{});
+      else launch(Tile64x128{}, Tile256{}, Store{});
+    }
+  }
+  if (w2.splits > 1) add_parts(w2, w1, 2, dtype, st);
 }
 
 uint32_t magic_of(int k) { return k > 1 ? (uint32_t)((0x100000000ull + (uint64_t)k - 1) / (uint64_t)k) : 0u; }
@@ -679,26 +607,34 @@ extern "C" int moe_ragged_gemm(const void* x, int dtype, int64_t S, const int32_
   return check_launch();
 }
 
-extern "C" size_t moe_ragged_wgrad_workspace_bytes(int, int64_t, int, int, int) { return 0; }
+extern "C" size_t moe_ragged_wgrad_workspace_bytes(int dtype, int64_t R, int E, int K, int N) {
+  if (check_product(dtype, R, E, K, N) != MOE_OK) return 0;
+  return part_bytes(weight_parts(dtype, R, E, K, N, 1), E, K, N);
+}
 
 extern "C" int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* dY, const int32_t* offsets,
-                                int64_t R, int E, int K, int N, void* dW, void*, size_t, void* stream) {
+                                int64_t R, int E, int K, int N, void* dW, void* ws, size_t ws_bytes, void* stream) {
   if (int rc = check_product(dtype, R, E, K, N)) return rc;
   if (int rc = check_source(x, dtype, S, inv, k, K)) return rc;
   MOE_REQUIRE_PTR(dY); MOE_REQUIRE_PTR(offsets); MOE_REQUIRE_PTR(dW);
+  const int parts = weight_parts(dtype, R, E, K, N, 1);
+  MOE_REQUIRE(parts == 1 || (ws != nullptr && ws_bytes >= part_bytes(parts, E, K, N)), MOE_EWORKSPACE);
+  MOE_OPTIONAL_PTR(ws);
   RaggedArgs a = base_args(offsets, R, E);
+  a.splits = parts;
   set_gather(a, inv, k, S);
   a.A = x; a.lda = K;
   a.B = dY; a.ldb = N;
   a.C = dW; a.ldc = N; a.c_goff = (int64_t)K * N;
   a.Mdim = K; a.Ndim = N; a.Kdim = a.R;
-  launch_weights(a, dtype, (hipStream_t)stream);
+  launch_weights(a, dtype, (float*)ws, (hipStream_t)stream);
   return check_launch();
 }
 
 extern "C" size_t moe_ragged_ffn_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp, int backward) {
   if (check_ffn(dtype, R, E, M, H, 0, n_esp) != MOE_OK) return 0;
-  return backward ? 2 * hidden_bytes(dtype, R, H / n_esp) : 0;
+  const int Hl = H / n_esp;
+  return backward ? 2 * hidden_bytes(dtype, R, Hl) + 2 * part_bytes(weight_parts(dtype, R, E, M, Hl, 2), E, M, Hl) : 0;
 }
 
 extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* W1, const void* W2,
@@ -740,7 +676,8 @@ extern "C" int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int6
   MOE_REQUIRE_PTR(dX); MOE_REQUIRE_PTR(dW1); MOE_REQUIRE_PTR(dW2);
   const int Hl = H / n_esp;
   const size_t hidden = hidden_bytes(dtype, R, Hl);
-  MOE_REQUIRE(ws != nullptr && ws_bytes >= 2 * hidden, MOE_EWORKSPACE);
+  const int parts = weight_parts(dtype, R, E, M, Hl, 2);
+  MOE_REQUIRE(ws != nullptr && ws_bytes >= 2 * hidden + 2 * part_bytes(parts, E, M, Hl), MOE_EWORKSPACE);
   MOE_REQUIRE(aligned16(ws), MOE_EALIGN);
   hipStream_t st = (hipStream_t)stream;
   const int64_t h0 = (int64_t)esp_idx * Hl;
@@ -760,14 +697,13 @@ extern "C" int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int6
   dx.B = W1; dx.ldb = H; dx.b_goff = (int64_t)M * H; dx.b_off = h0;
   dx.C = dX; dx.ldc = M;
   dx.Mdim = dx.R; dx.Ndim = M; dx.Kdim = Hl;
-  launch_rows<KIND_NT, EPI_STORE>(dx, dtype, st);
   // dW2[h0:h0+Hl, :] = Act^T dY
   RaggedArgs w2 = base_args(offsets, R, E);
   w2.A = Act; w2.lda = Hl;
   w2.B = dY; w2.ldb = M;
   w2.C = dW2; w2.ldc = M; w2.c_goff = (int64_t)H * M; w2.c_off = h0 * M;
   w2.Mdim = Hl; w2.Ndim = M; w2.Kdim = w2.R;
-  launch_weights(w2, dtype, st);
+  w2.splits = parts;
   // dW1[:, h0:h0+Hl] = X^T dZ
   RaggedArgs w1 = base_args(offsets, R, E);
   set_gather(w1, inv, k, S);
@@ -775,6 +711,7 @@ extern "C" int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int6
   w1.B = dZ; w1.ldb = Hl;
   w1.C = dW1; w1.ldc = H; w1.c_goff = (int64_t)M * H; w1.c_off = h0;
   w1.Mdim = M; w1.Ndim = Hl; w1.Kdim = w1.R;
-  launch_weights(w1, dtype, st);
+  w1.splits = parts;
+  launch_backward(dx, w2, w1, dtype, (float*)((char*)ws + 2 * hidden), st);
   return check_launch();
 }

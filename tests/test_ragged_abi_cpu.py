@@ -138,6 +138,6 @@ def test_polynomial_is_the_fitted_one():
     spec = importlib.util.spec_from_file_location("fit_gelu_poly", os.path.join(CSRC, "fit_gelu_poly.py"))
     fit = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(fit)
-    body = re.search(r"PHI_ODD\[\d+\] = \{([^}]*)\}", open(os.path.join(CSRC, "ragged.hip")).read()).group(1)
+    body = re.search(r"PHI_ODD\[\d+\] = \{([^}]*)\}", open(os.path.join(CSRC, "ragged.h")).read()).group(1)
     table = np.array([float(t.strip().rstrip("f")) for t in body.split(",")], dtype=np.float32)
     np.testing.assert_allclose(table, fit.tables()[0], rtol=2e-6)
