@@ -337,7 +337,9 @@ int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32_t* inv, in
  *     dX [R, M];  dW1, dW2 FULL tensors, only the shard's columns / rows are written
  * The kept form takes 1 + 1/32 bytes a hidden value, where moe_expert_ffn_fwd's Z and A take 4 (bf16)
  * or 8; the backward pass recomputes A.  Rows of Zq, Zs and A behind offsets[E] are not written.
- * Workspace: backward, dZ and the recomputed activation. */
+ * Workspace: backward, dZ, the recomputed activation and fp32 parts of the weight gradients where their
+ * reductions are split; forward, where nothing is kept and the rows are few, fp32 parts of the second
+ * product (without that room it takes the kernels for many rows). */
 size_t moe_ragged_ffn_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp,
                                       int backward);
 

@@ -113,6 +113,10 @@ __device__ __forceinline__ void gelu_and_grad_fast(float z, float& g, float& dg)
   dg = fmaf(z * 0.39894228040143267794f, __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f), cdf);   // (1/2) log2(e)
 }
 
+// The FFN of few rows (ragged_few.hip): bf16, nothing kept for a backward pass; ws of few_rows_bytes().
+size_t few_rows_bytes(int64_t R, int E, int M, int Hl);
+void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, void* ws, hipStream_t st);
+
 // fp32 products on the fp32 matrix cores (ragged_f32.hip); weight gradients with a.splits parts where EPI is EPI_PART
 constexpr int F32_TILE = 64;
 template <int KIND, int EPI>

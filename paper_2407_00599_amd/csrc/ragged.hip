@@ -388,16 +388,24 @@ void buffer_sizes(RaggedArgs& a, bool weights) {
   a.b_bytes = weights ? (uint64_t)a.R * (uint64_t)a.ldb * 2 : (uint64_t)a.G * (uint64_t)a.b_goff * 2;
 }
 
-TilePlan plan_rows(const RaggedArgs& a, bool wide = false) {   // wide: only tiles of eight waves
-  const float nk = (float)((a.Kdim + DK - 1) / DK), cu = (float)num_cus();
+// The tile of a bf16 row-tiled GEMM: the prices of the padded calls' tiles (ffn_tile.h) for what is multiplied, against the time of reading the
+// weights, 4.9 TB/s, of which a second row tile of an expert finds half in a cache.  Weights bound the launch where experts have few rows, and a tile that
+// all rows of most experts fit in is then the fastest: 8 experts of 64 rows x 4096 x 14336 and x 14336 x 4096, tiles of 128 x 128 189 and 188 us,
+// 64 x 128 198 and 243, 64 x 64 227 and 249; of 1024 x 1024 x 4096 102 and 128, 192 x 256 82.
+// wide: only tiles of eight waves.
+TilePlan plan_rows(const RaggedArgs& a, bool wide = false) {
+  const float nk = (float)((a.Kdim + DK - 1) / DK), cu = (float)num_cus(), used = (float)std::min(a.R, a.G);
+  const float weights = used * (float)a.Kdim * (float)a.Ndim * 2.f / 4.9e6f;
   TilePlan best{256, 256};
   float best_t = 0.f;
   for (const TileCost& c : ROW_TILES) {
     if (wide && c.tile.tile_n == 64) continue;
-    const float n = (float)(priced_row_tiles(a.R, a.G, c.tile.tile_m) * ((a.Ndim + c.tile.tile_n - 1) / c.tile.tile_n));
+    const float row_tiles = (float)priced_row_tiles(a.R, a.G, c.tile.tile_m);
+    const float n = row_tiles * (float)((a.Ndim + c.tile.tile_n - 1) / c.tile.tile_n);
     const float busy = c.per_cu == 1 ? n / cu : (n - cu) / cu;
     const float k = c.k_few + (c.k_all - c.k_few) * fminf(fmaxf(busy, 0.f), 1.f);
-    const float t = ceilf(n / (cu * c.per_cu)) * (nk * k + c.fixed);
+    const float products = ceilf(n / (cu * c.per_cu)) * (nk * k + c.fixed), reads = weights * 0.5f * (1.f + fmaxf(row_tiles / used, 1.f));
+    const float t = fmaxf(products, reads) + 0.2f * fminf(products, reads);
     if (best_t == 0.f || t < best_t) { best_t = t; best = c.tile; }
   }
   return best;
@@ -569,6 +577,14 @@ int check_ffn(int dtype, int64_t R, int E, int M, int H, int esp_idx, int n_esp)
   if (dtype == MOE_BF16) MOE_REQUIRE((uint64_t)M * H * 2 <= 0xFFFFFFF0ull, MOE_EUNSUPPORTED);
   return MOE_OK;
 }
+// The FFN of few rows (ragged_few.hip), where weights of a million values and more outweigh its launches and the second product's reduction is at
+// least twice as long as its rows are wide, which gives the tiles few workgroups.  Forward call, tiles and this: 8 experts x 1024 x 4096, 2 rows 28.5
+// and 17.6 us, 64 rows 44.0 and 38.5, 80 rows 44.3 and 45.3; one expert, 16 rows 30.2 and 20.7, 32 rows 31.7 and 27.8, 64 rows 30.4 and
+// 40.7; 8 x 512 x 2048, 64 rows 20.8 and 19.0; 8 x 256 x 1024, 64 rows 12.6 and 15.9; 8 x 1024 x 1024, 64 rows 18.4 and 21.5; 32 x 4096 x
+// 2048, 4 rows 32.3 and 39.4.
+bool few_rows(int dtype, int64_t R, int E, int M, int Hl) {
+  return dtype == MOE_BF16 && (R <= 8 * (int64_t)E || R <= 32) && Hl >= 2 * (int64_t)M && (int64_t)M * Hl >= 1 << 20;
+}
 size_t hidden_bytes(int dtype, int64_t R, int Hl) { return align_up((size_t)R * Hl * (dtype == MOE_BF16 ? 2 : 4), 256); }
 
 }  // namespace
@@ -634,17 +650,18 @@ extern "C" int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32
 extern "C" size_t moe_ragged_ffn_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp, int backward) {
   if (check_ffn(dtype, R, E, M, H, 0, n_esp) != MOE_OK) return 0;
   const int Hl = H / n_esp;
-  return backward ? 2 * hidden_bytes(dtype, R, Hl) + 2 * part_bytes(weight_parts(dtype, R, E, M, Hl, 2), E, M, Hl) : 0;
+  if (backward) return 2 * hidden_bytes(dtype, R, Hl) + 2 * part_bytes(weight_parts(dtype, R, E, M, Hl, 2), E, M, Hl);
+  return few_rows(dtype, R, E, M, Hl) ? few_rows_bytes(R, E, M, Hl) : 0;
 }
 
 extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* W1, const void* W2,
                                   const int32_t* offsets, int64_t R, int E, int M, int H, int esp_idx, int n_esp, void* Zq, void* Zs,
-                                  void* A, void* Y, void*, size_t, void* stream) {
+                                  void* A, void* Y, void* ws, size_t ws_bytes, void* stream) {
   if (int rc = check_ffn(dtype, R, E, M, H, esp_idx, n_esp)) return rc;
   if (int rc = check_source(x, dtype, S, inv, k, M)) return rc;
   MOE_REQUIRE_PTR(W1); MOE_REQUIRE_PTR(W2); MOE_REQUIRE_PTR(offsets); MOE_REQUIRE_PTR(A); MOE_REQUIRE_PTR(Y);
   MOE_REQUIRE((Zq == nullptr) == (Zs == nullptr), MOE_ENULL);
-  MOE_OPTIONAL_PTR(Zq); MOE_OPTIONAL_PTR(Zs);
+  MOE_OPTIONAL_PTR(Zq); MOE_OPTIONAL_PTR(Zs); MOE_OPTIONAL_PTR(ws);
   hipStream_t st = (hipStream_t)stream;
   const int Hl = H / n_esp;
   const int64_t h0 = (int64_t)esp_idx * Hl;
@@ -654,13 +671,19 @@ extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int
   a.B = W1; a.ldb = H; a.b_goff = (int64_t)M * H; a.b_off = h0;
   a.C = A; a.C2 = Zq; a.Zs = (uint8_t*)Zs; a.ldc = Hl; a.ldz = (Hl + 31) / 32;
   a.Mdim = a.R; a.Ndim = Hl; a.Kdim = M;
-  if (Zq) launch_rows<KIND_NN, EPI_GELU8>(a, dtype, st);
-  else launch_rows<KIND_NN, EPI_ACT>(a, dtype, st);
   RaggedArgs y = base_args(offsets, R, E);
   y.A = A; y.lda = Hl;
   y.B = W2; y.ldb = M; y.b_goff = (int64_t)H * M; y.b_off = h0 * M;
   y.C = Y; y.ldc = M;
   y.Mdim = y.R; y.Ndim = M; y.Kdim = Hl;
+  if (Zq == nullptr && few_rows(dtype, R, E, M, Hl) && ws != nullptr && ws_bytes >= few_rows_bytes(R, E, M, Hl)) {
+    buffer_sizes(a, false);
+    buffer_sizes(y, false);
+    launch_few_rows(a, y, ws, st);
+    return check_launch();
+  }
+  if (Zq) launch_rows<KIND_NN, EPI_GELU8>(a, dtype, st);
+  else launch_rows<KIND_NN, EPI_ACT>(a, dtype, st);
   launch_rows<KIND_NN, EPI_STORE>(y, dtype, st);
   return check_launch();
 }

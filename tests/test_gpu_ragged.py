@@ -170,6 +170,9 @@ FFN = [   # rows per expert, rows behind, M, H, n_esp, esp_idx, gather
     ((64, 33, 0, 100), 0, 72, 1032, 1, 0, False), ((150, 70), 40, 264, 520, 1, 0, True), ((3,) * 66, 0, 64, 40, 1, 0, True),
     ((400, 90, 513), 30, 128, 768, 4, 2, True), ((12,) * 8, 0, 512, 1024, 1, 0, True),
     ((2100, 0, 2600), 20, 64, 72, 1, 0, True), ((3200,), 0, 72, 136, 1, 0, False),     # weight gradients in parts
+    # few rows of large experts: a row, an expert with more rows than go along with one reading, experts without any, a shard
+    ((1,), 0, 512, 2048, 1, 0, True), ((0, 3, 0, 0, 1, 0, 7, 0), 3, 520, 2200, 1, 0, True), ((40, 0, 1, 0, 2, 0, 0), 5, 512, 4160, 2, 1, True),
+    ((20,), 2, 264, 4096, 1, 0, False), ((0,) * 65 + (3, 0, 2), 1, 136, 8200, 1, 0, True),
 ]
 
 
