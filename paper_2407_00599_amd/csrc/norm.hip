@@ -11,7 +11,9 @@
 // values: no cancellation), in fp32.  TPR threads hold a row, NV pieces of 8 values each; a workgroup walks over rows with the weights
 // in registers, because weights read again for every row would be more L2 traffic than the rows themselves (4 + 4 bytes a column
 // against 2).  Column sums stay in a thread's registers over all of its workgroup's rows, and the workgroups' sums are added in a
-// launch of their own in a fixed order: no atomics, the same bits every time.
+// launch of their own in a fixed order: no atomics, the same bits every time.  A workgroup's next row is requested before the current
+// one's sums, or 8 waves on a compute unit that stand at a barrier leave the memory idle.  bf16, 32768 rows of 4096, without and with that: n(x) 125 and 103 us
+// (5.2 TB/s), behind the block 155 and 149 (5.4), backward 219 and 195 (5.5), behind the block 208 and 170 (4.7); a copy runs at 4.9.
 #include <algorithm>
 #include <type_traits>
 
@@ -33,15 +35,32 @@ struct NormArgs {
   float alpha, eps;
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const void* base, int64_t at, float (&f)[8]) {
-  if constexpr (sizeof(T) == 2) {
-    unpack_bf16x8(*reinterpret_cast<const uint4*>((const bf16_t*)base + at), f);
-  } else {
-    const float4 a = *reinterpret_cast<const float4*>((const float*)base + at), b = *reinterpret_cast<const float4*>((const float*)base + at + 4);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  }
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
 }
+// eight values as they lie in memory: requested a row ahead, converted when they are used
+template <typename T>
+struct Raw8 {
+  u32x4_t q[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const void* base, int64_t at) {
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) q[h] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>((const T*)base + at) + h);
+  }
+  __device__ __forceinline__ void get(float (&f)[8]) const {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __uint_as_float(q[0][e] << 16);
+        f[2 * e + 1] = __uint_as_float(q[0][e] & 0xFFFF0000u);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(q[e / 4][e % 4]);
+    }
+  }
+};
 template <typename T>
 __device__ __forceinline__ void store8(void* base, int64_t at, const float (&f)[8]) {
   if constexpr (sizeof(T) == 2) {
@@ -56,6 +75,8 @@ constexpr int block_of(int tpr) { return tpr > 256 ? tpr : 256; }
 
 // Sums of N values over the TPR threads of a row, in every one of them.  `turn` alternates between two buffers, so that one
 // barrier a sum is enough.
+template <int TPR>
+constexpr int red_floats() { return TPR > 64 ? 2 * (block_of(TPR) / 64) * 4 : 1; }
 template <int TPR, int N>
 __device__ __forceinline__ void row_sums(float (&s)[N], float* red, int& turn) {
   constexpr int IN_WAVE = TPR < 64 ? TPR : 64, WAVES = TPR / 64;
@@ -64,18 +85,19 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float* red, int& turn) {
 #pragma unroll
     for (int d = 1; d < IN_WAVE; d <<= 1) s[n] += __shfl_xor(s[n], d, 64);
   if constexpr (WAVES > 1) {
-    float* r = red + turn * (WAVES * 4);
+    float* r = red + turn * (block_of(TPR) / 64 * 4);
     turn ^= 1;
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
       for (int n = 0; n < N; ++n) r[(threadIdx.x >> 6) * 4 + n] = s[n];
     }
     __syncthreads();
+    const int first = threadIdx.x / TPR * WAVES;      // the row's first wave
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       s[n] = 0.f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) s[n] += r[w * 4 + n];
+      for (int w = 0; w < WAVES; ++w) s[n] += r[(first + w) * 4 + n];
     }
   }
 }
@@ -84,7 +106,8 @@ __device__ __forceinline__ void row_sums(float (&s)[N], float* red, int& turn) {
 template <typename T, int TPR, int NV, bool RES>
 __global__ __launch_bounds__(block_of(TPR)) void norm_fwd(const NormArgs p) {
   constexpr int GROUPS = block_of(TPR) / TPR;
-  __shared__ float red[TPR > 64 ? 2 * (TPR / 64) * 4 : 1];
+  constexpr bool AHEAD = TPR < 1024;     // the next row's requests go out before this row's sums; 1024 threads have no registers for that
+  __shared__ float red[red_floats<TPR>()];
   const int lane = threadIdx.x % TPR, M = p.M;
   int turn = 0;
   float w[NV][8], b[NV][8], gc[RES ? NV : 1][8];
@@ -96,25 +119,38 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_fwd(const NormArgs p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) { w[i][e] = 0.f; b[i][e] = 0.f; if (RES) gc[RES ? i : 0][e] = 1.f; }
     if (in[i]) {
-      load8<float>(p.w, c, w[i]);
-      if (p.b) load8<float>(p.b, c, b[i]);
-      if (RES && p.gate_kind == GATE_CHANNEL) load8<float>(p.gate, c, gc[RES ? i : 0]);
+      load8(p.w + c, w[i]);
+      if (p.b) load8(p.b + c, b[i]);
+      if (RES && p.gate_kind == GATE_CHANNEL) load8(p.gate + c, gc[RES ? i : 0]);
     }
   }
   const float rm = 1.f / (float)M;
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR; row < (p.S + GROUPS - 1) / GROUPS * GROUPS; row += (int64_t)gridDim.x * GROUPS) {
-    const bool here = row < p.S;     // the rows of a workgroup's groups end together (barriers)
+  // The rows of a workgroup's groups end together (barriers): a group behind the last row works on that one and stores nothing.
+  const int64_t step = (int64_t)gridDim.x * GROUPS, end = (p.S + GROUPS - 1) / GROUPS * GROUPS;
+  Raw8<T> nv[NV], nr[RES ? NV : 1];
+  auto request = [&](int64_t row) {      // a piece behind the row's end is fetched from its beginning
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t at = min(row, p.S - 1) * M + (in[i] ? (i * TPR + lane) * 8 : 0);
+      nv[i].load(p.v, at);
+      if (RES) nr[RES ? i : 0].load(p.res, at);
+    }
+  };
+  int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / TPR;
+  if (AHEAD) request(row);
+  for (; row < end; row += step) {
+    if (!AHEAD) request(row);
+    const bool here = row < p.S;
     const int64_t base = row * M + lane * 8;
     float v[NV][8], r[RES ? NV : 1][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      nv[i].get(v[i]);
+      if (RES) nr[RES ? i : 0].get(r[RES ? i : 0]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-      if (here && in[i]) {
-        load8<T>(p.v, base + (int64_t)i * TPR * 8, v[i]);
-        if (RES) load8<T>(p.res, base + (int64_t)i * TPR * 8, r[RES ? i : 0]);
-      }
+      for (int e = 0; e < 8; ++e) v[i][e] = in[i] ? v[i][e] : 0.f;
     }
+    if (AHEAD) request(row + step);
     float mean = 0.f;
     if (p.layer) {
       float s[1] = {0.f};
@@ -168,8 +204,9 @@ __device__ __forceinline__ void weight_grads(const NormArgs& p, int c, float a, 
 
 template <typename T, int TPR, int NV, bool RES>
 __global__ __launch_bounds__(block_of(TPR)) void norm_bwd(const NormArgs p) {
-  constexpr int BLOCK = block_of(TPR), GROUPS = BLOCK / TPR;
-  __shared__ float red[TPR > 64 ? 2 * (TPR / 64) * 4 : GROUPS * TPR * 8];
+  constexpr int GROUPS = block_of(TPR) / TPR;
+  constexpr bool AHEAD = TPR < 1024;
+  __shared__ float red[GROUPS > 1 ? GROUPS * TPR * 8 : red_floats<TPR>()];
   const int lane = threadIdx.x % TPR, group = threadIdx.x / TPR, M = p.M;
   int turn = 0;
   float w[NV][8], wb[RES ? NV : 1][8], gc[RES ? NV : 1][8], ca[NV][8], cb[NV][8];
@@ -181,34 +218,51 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_bwd(const NormArgs p) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) { w[i][e] = 0.f; ca[i][e] = cb[i][e] = 0.f; if (RES) { wb[RES ? i : 0][e] = 0.f; gc[RES ? i : 0][e] = 1.f; } }
     if (in[i]) {
-      load8<float>(p.w, c, w[i]);
-      if (RES && p.gate_kind == GATE_TOKEN && p.b) load8<float>(p.b, c, wb[RES ? i : 0]);
-      if (RES && p.gate_kind == GATE_CHANNEL) load8<float>(p.gate, c, gc[RES ? i : 0]);
+      load8(p.w + c, w[i]);
+      if (RES && p.gate_kind == GATE_TOKEN && p.b) load8(p.b + c, wb[RES ? i : 0]);
+      if (RES && p.gate_kind == GATE_CHANNEL) load8(p.gate + c, gc[RES ? i : 0]);
     }
   }
   const float rm = 1.f / (float)M;
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < (p.S + GROUPS - 1) / GROUPS * GROUPS; row += (int64_t)gridDim.x * GROUPS) {
+  const int64_t step = (int64_t)gridDim.x * GROUPS, end = (p.S + GROUPS - 1) / GROUPS * GROUPS;
+  Raw8<T> nv[NV], ng[NV], nr[RES ? 1 : NV];
+  float next_mean = 0.f, next_rstd = 0.f;
+  auto request = [&](int64_t row) {      // as in the forward pass
+    row = min(row, p.S - 1);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int64_t at = row * M + (in[i] ? (i * TPR + lane) * 8 : 0);
+      nv[i].load(p.v, at);
+      ng[i].load(p.up, at);
+      if (!RES && p.res) nr[RES ? 0 : i].load(p.res, at);
+    }
+    if (p.layer) next_mean = p.mean_in[row];
+    next_rstd = p.rstd_in[row];
+  };
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  if (AHEAD) request(row);
+  for (; row < end; row += step) {
+    if (!AHEAD) request(row);
     const bool here = row < p.S;
     const int64_t base = row * M + lane * 8;
     float v[NV][8], g[NV][8], r[RES ? 1 : NV][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      nv[i].get(v[i]);
+      ng[i].get(g[i]);
+      if (!RES && p.res) nr[RES ? 0 : i].get(r[RES ? 0 : i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = g[i][e] = 0.f;
-      if (here && in[i]) {
-        load8<T>(p.v, base + (int64_t)i * TPR * 8, v[i]);
-        load8<T>(p.up, base + (int64_t)i * TPR * 8, g[i]);
-        if (!RES && p.res) load8<T>(p.res, base + (int64_t)i * TPR * 8, r[RES ? 0 : i]);
-      }
+      for (int e = 0; e < 8; ++e) g[i][e] = here && in[i] ? g[i][e] : 0.f;
     }
-    const float mean = here && p.layer ? p.mean_in[row] : 0.f, rstd = here ? p.rstd_in[row] : 0.f;
+    const float mean = next_mean, rstd = next_rstd;
+    if (AHEAD) request(row + step);
     const float tg = RES && p.gate_kind == GATE_TOKEN && here ? p.gate[row] : 1.f;
     float s[3] = {0.f, 0.f, 0.f};     // sums of gw hat, of gw, and (gate per token) of alpha dy n
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float hat = in[i] ? (v[i][e] - mean) * rstd : 0.f;
+        const float hat = here && in[i] ? (v[i][e] - mean) * rstd : 0.f;
         float up = g[i][e];
         if (RES) {
           up *= p.alpha;
@@ -304,7 +358,10 @@ namespace {
 constexpr int MAX_M = 32768;
 constexpr int BWD_BLOCKS = 512;      // two workgroups to a compute unit
 
-int threads_per_row(int M) { return M <= 128 ? 16 : M <= 2048 ? 64 : M <= 8192 ? 256 : 1024; }
+// Threads to a row, and pieces to a thread (with_shape): no more than four pieces, whose weights and column sums still leave a SIMD two waves, and as few
+// threads as that allows, for what a row costs beside its bytes.  bf16, 32768 rows, the four calls: 1536 columns on 64 threads 39 / 57 / 102 / 99 us,
+// 128 39 / 55 / 88 / 78, 256 41 / 68 / 125 / 104; 1024 on 64 28 / 38 / 53 / 46, on 256 38 / 57 / 119 / 99.
+int threads_per_row(int M) { return M <= 128 ? 16 : M <= 1024 ? 64 : M <= 2048 ? 128 : M <= 8192 ? 256 : 1024; }
 int groups_of(int M) { return block_of(threads_per_row(M)) / threads_per_row(M); }
 int64_t fwd_blocks(int64_t S, int M) { return std::min<int64_t>((S + groups_of(M) - 1) / groups_of(M), 2048); }
 // a workgroup has at least 4 rows to a group, or its column sums would be as much traffic as its rows
@@ -317,7 +374,7 @@ void with_shape(int M, F&& f) {
   if (M <= 128) go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
   else if (M <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
   else if (M <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-  else if (M <= 2048) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+  else if (M <= 2048) go(integral_constant<int, 128>{}, integral_constant<int, 2>{});
   else if (M <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
   else if (M <= 8192) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
   else if (M <= 16384) go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
