@@ -6,7 +6,7 @@ combine, and the mirror image backward).  With all E experts local and the N_ESP
 one after the other on the same GPU it evaluates the whole layer ("closed world"), which is
 what the parity tests compare with the CPU checker.  Nothing of the method is computed here: every
 step is a library call and torch only owns the memory (MoERankShape.fill_stand_ins copies buffers where a
-collective would move them).
+collective would move them).  `DroplessBlock` is a whole block with every expert local and no capacity padding.
 """
 from __future__ import annotations
 
@@ -236,3 +236,84 @@ class MoERankShape:
     def step(self, fused=False):
         for name in (self.STEPS_FUSED if fused else self.STEPS):
             getattr(self, name)()
+
+
+class DroplessBlock:
+    """A dropless MoE block: y = x + alpha * gate * n2(MoE(n1(x))), every expert local, no capacity padding.
+
+    norm -> gate -> plan of the ragged rows -> expert FFN over them -> combine -> norm, gate, residual scale and residual, and the
+    mirror image backward.  The rows of all experts are one buffer of k blocks of S rows to the combine calls.  Between forward and
+    backward the block keeps, per token and hidden column, one byte of pre-activation and a scale byte per 32; `infer` keeps nothing.
+
+    params: w1, b1, w2, b2 (norm weights, fp32 [M]; the biases only for "layer"), Wg [M, E] fp32, W1 [E, M, H], W2 [E, H, M], and
+    gate: fp32 [M] ("channel"), [S] ("token") or None."""
+
+    def __init__(self, S, M, H, E, k, dtype=torch.bfloat16, norm="rms", gate="none", alpha=1.0, eps=1e-5, norm_topk=-1,
+                 device="cuda:0"):
+        self.S, self.M, self.H, self.E, self.k = S, M, H, E, k
+        self.alpha, self.eps, self.norm_topk = alpha, eps, norm_topk
+        self.layer = norm == "layer"
+        self.kind = api.MOE_NORM_LAYER if self.layer else api.MOE_NORM_RMS
+        self.gate_kind = {"none": api.MOE_GATE_NONE, "channel": api.MOE_GATE_CHANNEL, "token": api.MOE_GATE_TOKEN}[gate]
+        self.R = R = S * k
+        i32, f32 = torch.int32, torch.float32
+        e = lambda *shape, dt=dtype: torch.empty(shape, dtype=dt, device=device)
+        self.code = api.MOE_BF16 if dtype == torch.bfloat16 else api.MOE_F32
+        self.u, self.h, self.y = e(S, M), e(S, M), e(S, M)
+        self.mean1, self.rstd1, self.mean2, self.rstd2 = (e(S, dt=f32) for _ in range(4))
+        self.logits = e(S, E, dt=f32); self.idx = e(S, k, dt=i32); self.slot = e(S, k, dt=i32)
+        self.w = e(S, k, dt=f32); self.inv = e(E, S, dt=i32); self.counts = e(E, dt=i32)
+        self.offsets = e(E + 1, dt=i32)
+        self.row_idx = e(S, k, dt=i32); self.row_slot = e(S, k, dt=i32); self.row_inv = e(k, S, dt=i32)
+        self.A = e(R, H); self.Y = e(R, M)
+        self.Zq = e(R, H, dt=torch.int8); self.Zs = e(R, (H + 31) // 32, dt=torch.uint8)
+        # backward
+        self.dh, self.du, self.dx = e(S, M), e(S, M), e(S, M)
+        self.dY, self.dX, self.dw = e(R, M), e(R, M), e(S, k, dt=f32)
+        self.dW1, self.dW2 = e(E, M, H), e(E, H, M)
+        self.dlogits = e(S, E, dt=f32); self.dWg = e(M, E, dt=f32)
+        self.dw1, self.db1, self.dw2, self.db2 = (e(M, dt=f32) for _ in range(4))
+        self.dgate = None if gate == "none" else e(M if gate == "channel" else S, dt=f32)
+        nbytes = max(api.moe_gate_workspace_bytes(S, E, k), api.moe_gate_bwd_workspace_bytes(S, M, E),
+                     api.moe_norm_bwd_workspace_bytes(S, M), 256,
+                     *(api.moe_ragged_ffn_workspace_bytes(self.code, R, E, M, H, 1, b) for b in (0, 1)))
+        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+    def _moe(self, x, p, keep):
+        S, M, E, k, R = self.S, self.M, self.E, self.k, self.R
+        stats = (lambda m, r: (m if self.layer else None, r)) if keep else (lambda m, r: (None, None))
+        b1, b2 = (p["b1"], p["b2"]) if self.layer else (None, None)
+        api.moe_norm_fwd(x, S, M, self.kind, p["w1"], b1, self.eps, self.u, *stats(self.mean1, self.rstd1))
+        # a token asks for an expert once: capacity S drops nothing
+        api.moe_gate_topk(self.u, p["Wg"], None, S, M, E, k, S, 0, 1, self.norm_topk, self.logits, self.idx, self.slot, self.w,
+                          self.inv, self.counts, self.ws)
+        api.moe_ragged_plan(self.idx, self.slot, self.counts, S, E, k, S, self.offsets, self.row_idx, self.row_slot, self.row_inv)
+        api.moe_ragged_ffn_fwd(self.u, S, self.row_inv, k, p["W1"], p["W2"], self.offsets, R, E, M, self.H, 0, 1,
+                               self.Zq if keep else None, self.Zs if keep else None, self.A, self.Y, self.ws)
+        api.moe_combine_fwd(self.Y, 1, S, M, k, k, S, self.row_idx, self.row_slot, self.w, self.h)
+        api.moe_norm_residual_fwd(self.h, x, S, M, self.kind, p["w2"], b2, p.get("gate"), self.gate_kind, self.alpha, self.eps,
+                                  self.y, *stats(self.mean2, self.rstd2))
+        return self.y
+
+    def infer(self, x, params):
+        return self._moe(x, params, keep=False)
+
+    def forward(self, x, params):
+        self.x, self.p = x, params
+        return self._moe(x, params, keep=True)
+
+    def backward(self, dy):
+        """dx; the gradients of the parameters are dw1, db1, dw2, db2, dgate, dWg, dW1, dW2."""
+        S, M, E, k, R, p = self.S, self.M, self.E, self.k, self.R, self.p
+        only = lambda t: t if self.layer else None
+        api.moe_norm_residual_bwd(dy, self.h, S, M, self.kind, p["w2"], only(p.get("b2")), p.get("gate"), self.gate_kind, self.alpha,
+                                  only(self.mean2), self.rstd2, self.dh, self.dw2, only(self.db2), self.dgate, self.ws)
+        api.moe_combine_bwd(self.dh, self.Y, 1, S, M, k, k, S, self.row_idx, self.row_slot, self.row_inv, self.w, self.dY, self.dw)
+        api.moe_ragged_ffn_bwd(self.dY, self.u, S, self.row_inv, k, self.Zq, self.Zs, p["W1"], p["W2"], self.offsets, R, E, M, self.H,
+                               0, 1, self.dX, self.dW1, self.dW2, self.ws)
+        api.moe_combine_fwd(self.dX, 1, S, M, k, k, S, self.row_idx, self.row_slot, None, self.du)
+        api.moe_gate_bwd(self.dw, self.w, self.idx, self.logits, self.u, p["Wg"], S, M, E, k, self.norm_topk, self.dlogits, self.dWg,
+                         None, self.du, 1, self.ws)
+        api.moe_norm_bwd(self.du, self.x, S, M, self.kind, p["w1"], only(self.mean1), self.rstd1, dy, self.dx, self.dw1,
+                         only(self.db1), self.ws)
+        return self.dx
