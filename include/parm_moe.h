@@ -304,7 +304,7 @@ int moe_gate_bwd(const float* dw, const float* w, const int32_t* idx, const floa
  *   W    [E, K, N], or with transposed = 1 [E, N, K]
  *   moe_ragged_gemm    Y [R, N] = X W of each row's expert; rows behind offsets[E] are zeros
  *   moe_ragged_wgrad   dW [E, K, N] = X^T dY over the expert's rows (zeros for an expert without)
- * fp32 accumulation.
+ * fp32 accumulation.  Workspace: fp32 parts of a reduction that is split because its tiles are few.
  * Limits: E <= 256, K and N multiples of 8, S*k and R at most 2^29, in bf16 x, Y and one expert's
  * matrix under 4 GiB each (MOE_EUNSUPPORTED).
  * --------------------------------------------------------------------------------------- */
@@ -338,8 +338,8 @@ int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32_t* inv, in
  * The kept form takes 1 + 1/32 bytes a hidden value, where moe_expert_ffn_fwd's Z and A take 4 (bf16)
  * or 8; the backward pass recomputes A.  Rows of Zq, Zs and A behind offsets[E] are not written.
  * Workspace: backward, dZ, the recomputed activation and fp32 parts of the weight gradients where their
- * reductions are split; forward, where nothing is kept and the rows are few, fp32 parts of the second
- * product (without that room it takes the kernels for many rows). */
+ * reductions are split; forward, fp32 parts of the second product where the rows are few (without that
+ * room it is not split and its sums are grouped differently). */
 size_t moe_ragged_ffn_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp,
                                       int backward);
 

@@ -117,8 +117,8 @@ __device__ __forceinline__ void gelu_and_grad_fast(float z, float& g, float& dg)
 size_t few_rows_bytes(int64_t R, int E, int M, int Hl);
 void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, void* ws, hipStream_t st);
 
-// fp32 products on the fp32 matrix cores (ragged_f32.hip); weight gradients with a.splits parts where EPI is EPI_PART
-constexpr int F32_TILE = 64;
+// fp32 products on the fp32 matrix cores (ragged_f32.hip); EPI_PART: the reduction in a.splits parts, which go to a.part
+constexpr int F32_TILE = 64, KC = 32;      // tile, k chunk
 template <int KIND, int EPI>
 void launch_f32(RaggedArgs a, hipStream_t st);
 void launch_trio_f32(RaggedArgs dx, RaggedArgs w2, RaggedArgs w1, hipStream_t st);

@@ -378,6 +378,19 @@ __global__ __launch_bounds__(256) void ragged_add_parts(const RaggedArgs p2, con
   else *reinterpret_cast<f32x4_t*>(dst) = v;
 }
 
+// The same for a split product over rows (fp32), whose rows behind the last expert's are zeros.
+__global__ __launch_bounds__(256) void ragged_add_rows(const RaggedArgs p) {
+  const int64_t size = (int64_t)p.R * p.Ndim, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (at >= size) return;
+  const int row = (int)(at / p.Ndim);
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (row < offset(p, p.G)) {
+#pragma unroll 4
+    for (int q = 0; q < p.splits; ++q) v += *reinterpret_cast<const f32x4_t*>(p.part + q * size + at);
+  }
+  *reinterpret_cast<f32x4_t*>(reinterpret_cast<float*>(p.C) + (int64_t)row * p.ldc + (at - (int64_t)row * p.Ndim)) = v;
+}
+
 // ------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------
@@ -423,6 +436,24 @@ void launch_kept_f32(RaggedArgs a, hipStream_t st) {
   else launch(integral_constant<int, 32>{}, std::false_type{});
 }
 
+// An fp32 product over rows with few tiles and a long reduction is cut into parts too, of at least ROW_PART_CHUNKS chunks of 32 k.
+constexpr int CHIP_CUS = 256;   // compute units of an MI355X
+constexpr int ROW_PART_CHUNKS = 8;
+int row_parts(int dtype, int64_t R, int E, int K, int N) {
+  if (dtype != MOE_F32) return 1;
+  const double tiles = priced_row_tiles((int)R, E, F32_TILE) * ((N + F32_TILE - 1) / F32_TILE);
+  const int parts = std::min({(int)(4 * CHIP_CUS / std::max(tiles, 1.0)), K / KC / ROW_PART_CHUNKS, 16});
+  return parts < 2 ? 1 : parts;
+}
+size_t row_part_bytes(int parts, int64_t R, int N) { return parts > 1 ? align_up((size_t)parts * R * N * 4, 256) : 0; }
+template <int KIND>
+void launch_row_parts(RaggedArgs a, int parts, void* ws, hipStream_t st) {
+  a.splits = parts;
+  a.part = (float*)ws;
+  launch_f32<KIND, EPI_PART>(a, st);
+  hipLaunchKernelGGL(ragged_add_rows, dim3((unsigned)(((int64_t)a.R * a.Ndim / 4 + 255) / 256)), dim3(256), 0, st, a);
+}
+
 template <int KIND, int EPI>
 void launch_rows(RaggedArgs a, int dtype, hipStream_t st) {
   if (dtype == MOE_F32) {
@@ -449,7 +480,6 @@ void launch_rows(RaggedArgs a, int dtype, hipStream_t st) {
 // thousands of rows is what a launch waits for: it is cut into parts of at least PART_TILES k tiles of an expert's mean share of the
 // rows, as many as the chip has room for (two workgroups of 128 x 128, four of fp32, to a compute unit).  Arithmetic on the shape: the parts
 // are a part of the workspace's size.
-constexpr int CHIP_CUS = 256;   // compute units of an MI355X
 constexpr int PART_TILES = 12;
 bool small_weights(int E, int M, int N) { return (int64_t)E * ((M + 255) / 256) * ((N + 255) / 256) < 64; }
 int weight_parts(int dtype, int64_t R, int E, int M, int N, int problems) {
@@ -604,21 +634,29 @@ extern "C" int moe_ragged_plan(const int32_t* idx, const int32_t* slot, const in
   return check_launch();
 }
 
-extern "C" size_t moe_ragged_gemm_workspace_bytes(int, int64_t, int, int, int) { return 0; }
+extern "C" size_t moe_ragged_gemm_workspace_bytes(int dtype, int64_t R, int E, int K, int N) {
+  if (check_product(dtype, R, E, K, N) != MOE_OK) return 0;
+  return row_part_bytes(row_parts(dtype, R, E, K, N), R, N);
+}
 
 extern "C" int moe_ragged_gemm(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* W, int transposed,
-                               const int32_t* offsets, int64_t R, int E, int K, int N, void* Y, void*, size_t, void* stream) {
+                               const int32_t* offsets, int64_t R, int E, int K, int N, void* Y, void* ws, size_t ws_bytes,
+                               void* stream) {
   if (int rc = check_product(dtype, R, E, K, N)) return rc;
   MOE_REQUIRE(transposed == 0 || transposed == 1, MOE_EINVAL);
   if (int rc = check_source(x, dtype, S, inv, k, K)) return rc;
   MOE_REQUIRE_PTR(W); MOE_REQUIRE_PTR(offsets); MOE_REQUIRE_PTR(Y);
+  const int parts = row_parts(dtype, R, E, K, N);
+  MOE_REQUIRE(parts == 1 || (ws != nullptr && ws_bytes >= row_part_bytes(parts, R, N)), MOE_EWORKSPACE);
+  MOE_OPTIONAL_PTR(ws);
   RaggedArgs a = base_args(offsets, R, E);
   set_gather(a, inv, k, S);
   a.A = x; a.lda = K;
   a.B = W; a.ldb = transposed ? K : N; a.b_goff = (int64_t)K * N;
   a.C = Y; a.ldc = N;
   a.Mdim = a.R; a.Ndim = N; a.Kdim = K;
-  if (transposed) launch_rows<KIND_NT, EPI_STORE>(a, dtype, (hipStream_t)stream);
+  if (parts > 1) transposed ? launch_row_parts<KIND_NT>(a, parts, ws, (hipStream_t)stream) : launch_row_parts<KIND_NN>(a, parts, ws, (hipStream_t)stream);
+  else if (transposed) launch_rows<KIND_NT, EPI_STORE>(a, dtype, (hipStream_t)stream);
   else launch_rows<KIND_NN, EPI_STORE>(a, dtype, (hipStream_t)stream);
   return check_launch();
 }
@@ -651,7 +689,7 @@ extern "C" size_t moe_ragged_ffn_workspace_bytes(int dtype, int64_t R, int E, in
   if (check_ffn(dtype, R, E, M, H, 0, n_esp) != MOE_OK) return 0;
   const int Hl = H / n_esp;
   if (backward) return 2 * hidden_bytes(dtype, R, Hl) + 2 * part_bytes(weight_parts(dtype, R, E, M, Hl, 2), E, M, Hl);
-  return few_rows(dtype, R, E, M, Hl) ? few_rows_bytes(R, E, M, Hl) : 0;
+  return few_rows(dtype, R, E, M, Hl) ? few_rows_bytes(R, E, M, Hl) : row_part_bytes(row_parts(dtype, R, E, Hl, M), R, M);
 }
 
 extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* W1, const void* W2,
@@ -684,7 +722,9 @@ extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int
   }
   if (Zq) launch_rows<KIND_NN, EPI_GELU8>(a, dtype, st);
   else launch_rows<KIND_NN, EPI_ACT>(a, dtype, st);
-  launch_rows<KIND_NN, EPI_STORE>(y, dtype, st);
+  const int parts = row_parts(dtype, R, E, Hl, M);
+  if (parts > 1 && ws != nullptr && ws_bytes >= row_part_bytes(parts, R, M)) launch_row_parts<KIND_NN>(y, parts, ws, st);
+  else launch_rows<KIND_NN, EPI_STORE>(y, dtype, st);
   return check_launch();
 }
 
