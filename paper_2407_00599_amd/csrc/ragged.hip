@@ -31,6 +31,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void ragged_plan(const int32_t* __res
                                                             int32_t* __restrict__ row_slot, int32_t* __restrict__ row_inv) {
   __shared__ int off[MOE_MAX_E + 1], wave_sum[PLAN_THREADS / 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int c = (int)blockIdx.x * PLAN_THREADS + tid;     // choice t k + j; and, for the empty rows, a row
+  const int e = idx[min(c, R - 1)], s = slot[min(c, R - 1)];      // requested with the counts, not behind their scan
   const int kept = tid < E ? min(max(counts[tid], 0), C) : 0;
   int incl = kept;
 #pragma unroll
@@ -45,11 +47,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void ragged_plan(const int32_t* __res
   if (tid == 0) off[0] = 0;
   __syncthreads();
   if (blockIdx.x == 0)
-    for (int e = tid; e <= E; e += PLAN_THREADS) offsets[e] = off[e];
+    for (int q = tid; q <= E; q += PLAN_THREADS) offsets[q] = off[q];
   const int end = off[E];
-  const int c = (int)blockIdx.x * PLAN_THREADS + tid;     // choice t k + j; and, for the empty rows, a row
   if (c >= R) return;
-  const int e = idx[c], s = slot[c];
   int row = -1;
   if (s >= 0 && (unsigned)e < (unsigned)E && s < off[e + 1] - off[e]) row = off[e] + s;
   row_idx[c] = row >= 0 ? (int)((unsigned)row / (unsigned)S) : 0;
