@@ -350,6 +350,8 @@ def moe_ragged_ffn_workspace_bytes(dtype, R, E, M, H, n_esp, backward) -> int:
 def moe_ragged_ffn_fwd(x, S, inv, k, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, Zq, Zs, A, Y, ws=None):
     wp, wb = _ws_args(ws)
     _typed(torch.int32, inv, offsets)
+    _typed(torch.int8, Zq)
+    _typed(torch.uint8, Zs)
     _check((_lib or lib()).moe_ragged_ffn_fwd(_ptr(x), _same_dtype(x, W1, W2, A, Y), S, _ptr(inv), k, _ptr(W1), _ptr(W2),
                                               _ptr(offsets), R, E, M, H, esp_idx, n_esp, _ptr(Zq), _ptr(Zs), _ptr(A),
                                               _ptr(Y), wp, wb, _stream()), "moe_ragged_ffn_fwd")
@@ -358,17 +360,23 @@ def moe_ragged_ffn_fwd(x, S, inv, k, W1, W2, offsets, R, E, M, H, esp_idx, n_esp
 def moe_ragged_ffn_bwd(dY, x, S, inv, k, Zq, Zs, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, dX, dW1, dW2, ws):
     wp, wb = _ws_args(ws)
     _typed(torch.int32, inv, offsets)
+    _typed(torch.int8, Zq)
+    _typed(torch.uint8, Zs)
     _check((_lib or lib()).moe_ragged_ffn_bwd(_ptr(dY), _ptr(x), _same_dtype(x, dY, W1, W2, dX, dW1, dW2), S, _ptr(inv), k,
                                               _ptr(Zq), _ptr(Zs), _ptr(W1), _ptr(W2), _ptr(offsets), R, E, M, H, esp_idx,
                                               n_esp, _ptr(dX), _ptr(dW1), _ptr(dW2), wp, wb, _stream()), "moe_ragged_ffn_bwd")
 
 
 def moe_ckpt8_store(x, rows, cols, q, scales):
+    _typed(torch.int8, q)
+    _typed(torch.uint8, scales)
     _check((_lib or lib()).moe_ckpt8_store(_ptr(x), dtype_code(x), rows, cols, _ptr(q), _ptr(scales), _stream()),
            "moe_ckpt8_store")
 
 
 def moe_ckpt8_load(q, scales, rows, cols, x):
+    _typed(torch.int8, q)
+    _typed(torch.uint8, scales)
     _check((_lib or lib()).moe_ckpt8_load(_ptr(q), _ptr(scales), rows, cols, _ptr(x), dtype_code(x), _stream()),
            "moe_ckpt8_load")
 
@@ -393,7 +401,7 @@ def moe_norm_bwd_workspace_bytes(S, M) -> int:
 def moe_norm_bwd(du, x, S, M, kind, w, mean, rstd, dres, dx, dw, db, ws):
     wp, wb = _ws_args(ws)
     _typed(torch.float32, w, mean, rstd, dw, db)
-    _check((_lib or lib()).moe_norm_bwd(_ptr(du), _ptr(x), _same_dtype(x, du, dx), S, M, kind, _ptr(w), _ptr(mean),
+    _check((_lib or lib()).moe_norm_bwd(_ptr(du), _ptr(x), _same_dtype(x, du, dx, *([] if dres is None else [dres])), S, M, kind, _ptr(w), _ptr(mean),
                                         _ptr(rstd), _ptr(dres), _ptr(dx), _ptr(dw), _ptr(db), wp, wb, _stream()),
            "moe_norm_bwd")
 

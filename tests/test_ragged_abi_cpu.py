@@ -131,6 +131,8 @@ def test_binding_refuses_mixed_types():
     with pytest.raises(ValueError):
         api.moe_ragged_plan(i, i, i, 1, 1, 1, 1, i, i, i, i)
     with pytest.raises(ValueError):
+        api.moe_ckpt8_store(f, 1, 8, i, torch.zeros(1, dtype=torch.uint8))      # the 8-bit values are int8
+    with pytest.raises(ValueError):
         api.moe_norm_fwd(h, 1, 8, api.MOE_NORM_RMS, h, None, 1e-5, h)     # weights are fp32
 
 
