@@ -17,7 +17,7 @@
 //
 // bf16 path: one kernel, MFMA (v_mfma_f32_16x16x32_bf16 in the two largest tiles but for weight gradients of few k tiles,
 // v_mfma_f32_32x32x16_bf16 in the others) with fp32 accumulation, over a family of tiles from 256 x 256 down to 32 x 64
-// (described in front of gemm_dma_tile; plan_tiles chooses).  Global memory goes straight to LDS (buffer_load ... lds) in
+// (described in front of gemm_dma_tile in ffn_tile.h; plan_tiles chooses).  Global memory goes straight to LDS (buffer_load ... lds) in
 // k tiles of 64; operands whose memory layout has k as the slow index stay in that layout in LDS and are read with the
 // transposing LDS load, so no transpose pass exists.  The MFMA is issued with the operands swapped (D^T = B^T A^T) so that a
 // lane ends up with 4 consecutive output columns.

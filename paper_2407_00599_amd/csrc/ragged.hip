@@ -436,7 +436,8 @@ void launch_kept_f32(RaggedArgs a, hipStream_t st) {
   else launch(integral_constant<int, 32>{}, std::false_type{});
 }
 
-// An fp32 product over rows with few tiles and a long reduction is cut into parts too, of at least ROW_PART_CHUNKS chunks of 32 k.
+// An fp32 product over rows with few tiles and a long reduction is cut into parts too, of at least ROW_PART_CHUNKS chunks of 32 k: 8 experts of
+// 256 rows x 2048 x 512 96 us whole, 68 in parts and 5 for adding them.
 constexpr int CHIP_CUS = 256;   // compute units of an MI355X
 constexpr int ROW_PART_CHUNKS = 8;
 int row_parts(int dtype, int64_t R, int E, int K, int N) {
@@ -478,8 +479,9 @@ void launch_rows(RaggedArgs a, int dtype, hipStream_t st) {
 
 // Weight gradients.  Tiles of 128 x 128 where those of 256 x 256 would be fewer than 64; of fp32, 64 x 64.  With few tiles a reduction over
 // thousands of rows is what a launch waits for: it is cut into parts of at least PART_TILES k tiles of an expert's mean share of the
-// rows, as many as the chip has room for (two workgroups of 128 x 128, four of fp32, to a compute unit).  Arithmetic on the shape: the parts
-// are a part of the workspace's size.
+// rows, as many as the chip has room for (two workgroups of 128 x 128, four of fp32, to a compute unit).  Whole and in parts, bf16 (fp32): 4 experts of
+// 4096 rows x 256 x 512 50 and 22 us (134 and 72), 2 of 16384 x 512 x 128 178 and 23 (512 and 69), 1 of 8192 x 1024 x 1024 92 and 38 (266 and
+// 192), 8 of 2048 x 128 x 256 23 and 19 (67 and 39).  Arithmetic on the shape: the parts are a part of the workspace's size.
 constexpr int PART_TILES = 12;
 bool small_weights(int E, int M, int N) { return (int64_t)E * ((M + 255) / 256) * ((N + 255) / 256) < 64; }
 int weight_parts(int dtype, int64_t R, int E, int M, int N, int problems) {
