@@ -171,12 +171,16 @@ struct Ragged {
         }
       }
     auto half = [](uint32_t o) { return o == OOB ? OOB : o >> 1; };       // the same place in the 8-bit values
-    // scales of this lane's row (accumulator order, group h of block i): offset of the first of its NBK blocks, or OOB
+    // scales of this lane's row (accumulator order, group h of block i): offset of the first of its NBK blocks (+ S_ZERO: a row of zeros, whose
+    // accumulators are another row's), or OOB; offsets are under 2^28, a block being 8 columns at least
+    constexpr uint32_t S_ZERO = 1u << 30;
     uint32_t s_off[Q_OUT || Q_IN ? MB : 1][RG];
     if constexpr (Q_OUT || Q_IN) {
       uint32_t mine[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) mine[u] = out_off[u] == OOB ? OOB : (out_off[u] >> 1) / (uint32_t)p.ldc * (uint32_t)p.ldz + (uint32_t)(nbase >> 5);
+      for (int u = 0; u < 2; ++u)
+        mine[u] = out_off[u] == OOB ? OOB
+                                    : ((out_off[u] >> 1) / (uint32_t)p.ldc * (uint32_t)p.ldz + (uint32_t)(nbase >> 5)) | (Q_OUT && (out_off[u] & 1u) ? S_ZERO : 0u);
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
@@ -186,7 +190,7 @@ struct Ragged {
         }
     }
     auto s_at = [&](int i, int h, int j) -> uint32_t {
-      return s_off[i][h] != OOB && nbase + 32 * j < p.Ndim ? s_off[i][h] + j : OOB;
+      return s_off[i][h] != OOB && nbase + 32 * j < p.Ndim ? (Q_OUT ? s_off[i][h] & ~S_ZERO : s_off[i][h]) + j : OOB;
     };
     u32x2_t q_next[Q_IN ? NT : 1];
     uint32_t s_next[RG][NBK];
@@ -242,7 +246,7 @@ struct Ragged {
             }
 #pragma unroll
             for (int d = MR; d < 64; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
-            b = ckpt8_scale(top);
+            b = s_off[i][h] & S_ZERO ? 0 : ckpt8_scale(top);
             if (lane < MR) __builtin_amdgcn_raw_buffer_store_b8((unsigned char)b, rS, (int)s_at(i, h, j), 0, 2);
           } else if constexpr (Q_IN) {
             b = (int)sv[h][j];
