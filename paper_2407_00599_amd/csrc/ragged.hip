@@ -296,9 +296,16 @@ struct Ragged {
     }
   }
 
+  // Bits of |z| rounded towards zero: ckpt8_scale's borders are fp32 values, so it decides them as for z itself.  What fp32's own
+  // rounding makes an infinity stays one.
+  static __device__ __forceinline__ uint32_t magnitude_below(double z) {
+    const float f = fabsf((float)z);
+    const uint32_t bits = __float_as_uint(f);
+    return bits < 0x7F800000u && (double)f > fabs(z) ? bits - 1u : bits;
+  }
   // Epilogue of the fp32 tile: lane l holds D[4 r + l / 16][l % 16] of its blocks of 16 columns, in fp64.  For the 8-bit form the tile
-  // goes through LDS, because two waves share a row where the k halves are split; it is formed from the fp64 sums, whose rounding to
-  // fp32 could move a value across the border between two steps.
+  // goes through LDS, because two waves share a row where the k halves are split; values and scales are formed from the fp64 sums, whose rounding to
+  // fp32 could move one across the border between two steps.
   template <int KIND, int EPI, int TM, int TN, int KW>
   static __device__ __forceinline__ void store_f32(const Args& p, const f64x4_t (&acc)[TN / 16], double* Bs, int g, int m0, int n0,
                                                    int rw, int kw, int lane, int o_row, bool o_zero) {
@@ -321,7 +328,7 @@ struct Ragged {
 #pragma unroll
     for (int u = 0; u < CPT; ++u) {
       z[u] = zero || n + u >= p.Ndim ? 0.0 : Bs[ml * PITCH + c0 + u];
-      top = max(top, __float_as_uint((float)z[u]) & 0x7FFFFFFFu);
+      top = max(top, magnitude_below(z[u]));
     }
 #pragma unroll
     for (int d = 1; d < TPU; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d, 64));
