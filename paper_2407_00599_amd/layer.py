@@ -10,6 +10,8 @@ collective would move them).  `DroplessBlock` is a whole block with every expert
 """
 from __future__ import annotations
 
+from types import SimpleNamespace
+
 import torch
 
 from . import api
@@ -242,14 +244,19 @@ class DroplessBlock:
     """A dropless MoE block: y = x + alpha * gate * n2(MoE(n1(x))), every expert local, no capacity padding.
 
     norm -> gate -> plan of the ragged rows -> expert FFN over them -> combine -> norm, gate, residual scale and residual, and the
-    mirror image backward.  The rows of all experts are one buffer of k blocks of S rows to the combine calls.  Between forward and
-    backward the block keeps, per token and hidden column, one byte of pre-activation and a scale byte per 32; `infer` keeps nothing.
+    mirror image backward.  The rows of all experts are one buffer of k blocks of S rows to the combine calls.
+
+    `forward` keeps what `backward` reads in the block's buffers until the next `forward`: of the hidden layer one byte of pre-activation a
+    value and a scale byte per 32, for each of the S k rows; beside it the experts' rows, the routing, u, h and the statistics.  x and
+    the parameters are kept by reference.  `infer` keeps nothing and has buffers of its own for what it writes (the activation [S k, H] and the
+    workspace are scratch of every call), so it may run between `forward` and `backward`.  Each returns a buffer that its next
+    call overwrites.  training=False: a block that only serves, without the gradients' and the kept buffers.
 
     params: w1, b1, w2, b2 (norm weights, fp32 [M]; the biases only for "layer"), Wg [M, E] fp32, W1 [E, M, H], W2 [E, H, M], and
     gate: fp32 [M] ("channel"), [S] ("token") or None."""
 
     def __init__(self, S, M, H, E, k, dtype=torch.bfloat16, norm="rms", gate="none", alpha=1.0, eps=1e-5, norm_topk=-1,
-                 device="cuda:0"):
+                 device="cuda:0", training=True):
         self.S, self.M, self.H, self.E, self.k = S, M, H, E, k
         self.alpha, self.eps, self.norm_topk = alpha, eps, norm_topk
         self.layer = norm == "layer"
@@ -259,51 +266,62 @@ class DroplessBlock:
         i32, f32 = torch.int32, torch.float32
         e = lambda *shape, dt=dtype: torch.empty(shape, dtype=dt, device=device)
         self.code = api.MOE_BF16 if dtype == torch.bfloat16 else api.MOE_F32
-        self.u, self.h, self.y = e(S, M), e(S, M), e(S, M)
-        self.mean1, self.rstd1, self.mean2, self.rstd2 = (e(S, dt=f32) for _ in range(4))
-        self.logits = e(S, E, dt=f32); self.idx = e(S, k, dt=i32); self.slot = e(S, k, dt=i32)
-        self.w = e(S, k, dt=f32); self.inv = e(E, S, dt=i32); self.counts = e(E, dt=i32)
-        self.offsets = e(E + 1, dt=i32)
-        self.row_idx = e(S, k, dt=i32); self.row_slot = e(S, k, dt=i32); self.row_inv = e(k, S, dt=i32)
-        self.A = e(R, H); self.Y = e(R, M)
-        self.Zq = e(R, H, dt=torch.int8); self.Zs = e(R, (H + 31) // 32, dt=torch.uint8)
-        # backward
-        self.dh, self.du, self.dx = e(S, M), e(S, M), e(S, M)
-        self.dY, self.dX, self.dw = e(R, M), e(R, M), e(S, k, dt=f32)
-        self.dW1, self.dW2 = e(E, M, H), e(E, H, M)
-        self.dlogits = e(S, E, dt=f32); self.dWg = e(M, E, dt=f32)
-        self.dw1, self.db1, self.dw2, self.db2 = (e(M, dt=f32) for _ in range(4))
-        self.dgate = None if gate == "none" else e(M if gate == "channel" else S, dt=f32)
-        nbytes = max(api.moe_gate_workspace_bytes(S, E, k), api.moe_gate_bwd_workspace_bytes(S, M, E),
-                     api.moe_norm_bwd_workspace_bytes(S, M), 256,
-                     *(api.moe_ragged_ffn_workspace_bytes(self.code, R, E, M, H, 1, b) for b in (0, 1)))
-        self.ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.A, self.inv = e(R, H), e(E, S, dt=i32)
 
-    def _moe(self, x, p, keep):
+        def written_by_a_pass():
+            return dict(u=e(S, M), h=e(S, M), y=e(S, M), Y=e(R, M), logits=e(S, E, dt=f32), idx=e(S, k, dt=i32), slot=e(S, k, dt=i32),
+                        w=e(S, k, dt=f32), counts=e(E, dt=i32), offsets=e(E + 1, dt=i32), row_idx=e(S, k, dt=i32),
+                        row_slot=e(S, k, dt=i32), row_inv=e(k, S, dt=i32))
+        self.serving = SimpleNamespace(**written_by_a_pass())
+        self.training, self.x = training, None
+        if training:
+            self.__dict__.update(written_by_a_pass())
+            self.mean1, self.rstd1, self.mean2, self.rstd2 = (e(S, dt=f32) for _ in range(4))
+            self.Zq = e(R, H, dt=torch.int8); self.Zs = e(R, (H + 31) // 32, dt=torch.uint8)
+            self.dh, self.du, self.dx = e(S, M), e(S, M), e(S, M)
+            self.dY, self.dX, self.dw = e(R, M), e(R, M), e(S, k, dt=f32)
+            self.dW1, self.dW2 = e(E, M, H), e(E, H, M)
+            self.dlogits = e(S, E, dt=f32); self.dWg = e(M, E, dt=f32)
+            self.dw1, self.db1, self.dw2, self.db2 = (e(M, dt=f32) for _ in range(4))
+            self.dgate = None if gate == "none" else e(M if gate == "channel" else S, dt=f32)
+        nbytes = [api.moe_gate_workspace_bytes(S, E, k), api.moe_ragged_ffn_workspace_bytes(self.code, R, E, M, H, 1, 0), 256]
+        if training:
+            nbytes += [api.moe_gate_bwd_workspace_bytes(S, M, E), api.moe_norm_bwd_workspace_bytes(S, M),
+                       api.moe_ragged_ffn_workspace_bytes(self.code, R, E, M, H, 1, 1)]
+        self.ws = torch.empty(max(nbytes), dtype=torch.uint8, device=device)
+
+    def _moe(self, x, p, t, keep):
+        """t: where the pass writes."""
         S, M, E, k, R = self.S, self.M, self.E, self.k, self.R
-        stats = (lambda m, r: (m if self.layer else None, r)) if keep else (lambda m, r: (None, None))
+        m1, r1, m2, r2 = (self.mean1, self.rstd1, self.mean2, self.rstd2) if keep else (None,) * 4
         b1, b2 = (p["b1"], p["b2"]) if self.layer else (None, None)
-        api.moe_norm_fwd(x, S, M, self.kind, p["w1"], b1, self.eps, self.u, *stats(self.mean1, self.rstd1))
+        if not self.layer:
+            m1 = m2 = None
+        api.moe_norm_fwd(x, S, M, self.kind, p["w1"], b1, self.eps, t.u, m1, r1)
         # a token asks for an expert once: capacity S drops nothing
-        api.moe_gate_topk(self.u, p["Wg"], None, S, M, E, k, S, 0, 1, self.norm_topk, self.logits, self.idx, self.slot, self.w,
-                          self.inv, self.counts, self.ws)
-        api.moe_ragged_plan(self.idx, self.slot, self.counts, S, E, k, S, self.offsets, self.row_idx, self.row_slot, self.row_inv)
-        api.moe_ragged_ffn_fwd(self.u, S, self.row_inv, k, p["W1"], p["W2"], self.offsets, R, E, M, self.H, 0, 1,
-                               self.Zq if keep else None, self.Zs if keep else None, self.A, self.Y, self.ws)
-        api.moe_combine_fwd(self.Y, 1, S, M, k, k, S, self.row_idx, self.row_slot, self.w, self.h)
-        api.moe_norm_residual_fwd(self.h, x, S, M, self.kind, p["w2"], b2, p.get("gate"), self.gate_kind, self.alpha, self.eps,
-                                  self.y, *stats(self.mean2, self.rstd2))
-        return self.y
+        api.moe_gate_topk(t.u, p["Wg"], None, S, M, E, k, S, 0, 1, self.norm_topk, t.logits, t.idx, t.slot, t.w, self.inv, t.counts, self.ws)
+        api.moe_ragged_plan(t.idx, t.slot, t.counts, S, E, k, S, t.offsets, t.row_idx, t.row_slot, t.row_inv)
+        api.moe_ragged_ffn_fwd(t.u, S, t.row_inv, k, p["W1"], p["W2"], t.offsets, R, E, M, self.H, 0, 1,
+                               self.Zq if keep else None, self.Zs if keep else None, self.A, t.Y, self.ws)
+        api.moe_combine_fwd(t.Y, 1, S, M, k, k, S, t.row_idx, t.row_slot, t.w, t.h)
+        api.moe_norm_residual_fwd(t.h, x, S, M, self.kind, p["w2"], b2, p.get("gate"), self.gate_kind, self.alpha, self.eps, t.y, m2, r2)
+        return t.y
 
     def infer(self, x, params):
-        return self._moe(x, params, keep=False)
+        return self._moe(x, params, self.serving, keep=False)
 
     def forward(self, x, params):
+        if not self.training:
+            raise RuntimeError("a block with training=False has no forward pass that is kept: use infer")
+        self.x = None                 # a call that is refused half way leaves nothing to go back through
+        y = self._moe(x, params, self, keep=True)
         self.x, self.p = x, params
-        return self._moe(x, params, keep=True)
+        return y
 
     def backward(self, dy):
         """dx; the gradients of the parameters are dw1, db1, dw2, db2, dgate, dWg, dW1, dW2."""
+        if self.x is None:
+            raise RuntimeError("backward without a forward pass")
         S, M, E, k, R, p = self.S, self.M, self.E, self.k, self.R, self.p
         only = lambda t: t if self.layer else None
         api.moe_norm_residual_bwd(dy, self.h, S, M, self.kind, p["w2"], only(p.get("b2")), p.get("gate"), self.gate_kind, self.alpha,
