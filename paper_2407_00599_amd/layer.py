@@ -255,13 +255,17 @@ class DroplessBlock:
     params: w1, b1, w2, b2 (norm weights, fp32 [M]; the biases only for "layer"), Wg [M, E] fp32, W1 [E, M, H], W2 [E, H, M], and
     gate: fp32 [M] ("channel"), [S] ("token") or None."""
 
+    NORMS = {"rms": api.MOE_NORM_RMS, "layer": api.MOE_NORM_LAYER}
+    GATES = {"none": api.MOE_GATE_NONE, "channel": api.MOE_GATE_CHANNEL, "token": api.MOE_GATE_TOKEN}
+
     def __init__(self, S, M, H, E, k, dtype=torch.bfloat16, norm="rms", gate="none", alpha=1.0, eps=1e-5, norm_topk=-1,
                  device="cuda:0", training=True):
         self.S, self.M, self.H, self.E, self.k = S, M, H, E, k
         self.alpha, self.eps, self.norm_topk = alpha, eps, norm_topk
+        if norm not in self.NORMS or gate not in self.GATES:
+            raise ValueError(f"norm is one of {list(self.NORMS)}, gate one of {list(self.GATES)}: got {norm!r}, {gate!r}")
         self.layer = norm == "layer"
-        self.kind = api.MOE_NORM_LAYER if self.layer else api.MOE_NORM_RMS
-        self.gate_kind = {"none": api.MOE_GATE_NONE, "channel": api.MOE_GATE_CHANNEL, "token": api.MOE_GATE_TOKEN}[gate]
+        self.kind, self.gate_kind = self.NORMS[norm], self.GATES[gate]
         self.R = R = S * k
         i32, f32 = torch.int32, torch.float32
         e = lambda *shape, dt=dtype: torch.empty(shape, dtype=dt, device=device)
