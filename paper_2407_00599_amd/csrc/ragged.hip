@@ -621,12 +621,16 @@ int check_ffn(int dtype, int64_t R, int E, int M, int H, int esp_idx, int n_esp)
   return MOE_OK;
 }
 // The FFN of few rows (ragged_few.hip), where weights of a million values and more outweigh its launches and the second product's reduction is at
-// least twice as long as its rows are wide, which gives the tiles few workgroups.  Forward call, tiles and this: 8 experts x 1024 x 4096, 2 rows 28.5
-// and 17.6 us, 64 rows 44.0 and 38.5, 80 rows 44.3 and 45.3; one expert, 16 rows 30.2 and 20.7, 32 rows 31.7 and 27.8, 64 rows 30.4 and
-// 40.7; 8 x 512 x 2048, 64 rows 20.8 and 19.0; 8 x 256 x 1024, 64 rows 12.6 and 15.9; 8 x 1024 x 1024, 64 rows 18.4 and 21.5; 32 x 4096 x
-// 2048, 4 rows 32.3 and 39.4.
+// least twice as long as its rows are wide, which gives the tiles few workgroups.  Forward call, tiles and this: 8 experts x 1024 x 4096, 2 rows 23.2
+// and 16.2 us, 64 rows 42.9 and 38.1; 8 x 2048 x 8192, 2 rows 54.2 and 39.4; 8 x 256 x 1024, 64 rows 12.6 and 15.9; 8 x 1024 x 1024, 64 rows 18.4 and
+// 21.5; 32 x 4096 x 2048, 4 rows 32.3 and 39.4.
+// An expert's weights are read again for every 16 rows, and how the rows are spread is not known here, so their number has a bound: up to 32 rows
+// this is the faster one or even under any routing, up to 64 it gains up to 12 % if the experts get equal shares and loses as much (8 x 1024 x 4096,
+// 64 rows) if their logits differ by N(0, 1) or N(0, 2), beyond it gains nothing and loses the more (E x 1024 x 4096, tiles and this, equal and skewed by N(0, 2): 16
+// experts, 128 rows 64.1 and 64.0, 40.7 and 66.2; 64 experts, 256 rows 195 and 196, 64 and 129; 512 rows 204 and 210, 78 and 258; one expert of 64 with all 512
+// rows 36 and 354).
 bool few_rows(int dtype, int64_t R, int E, int M, int Hl) {
-  return dtype == MOE_BF16 && (R <= 8 * (int64_t)E || R <= 32) && Hl >= 2 * (int64_t)M && (int64_t)M * Hl >= 1 << 20;
+  return dtype == MOE_BF16 && (R <= 32 || (R <= 64 && R <= 8 * (int64_t)E)) && Hl >= 2 * (int64_t)M && (int64_t)M * Hl >= 1 << 20;
 }
 size_t hidden_bytes(int dtype, int64_t R, int Hl) { return align_up((size_t)R * Hl * (dtype == MOE_BF16 ? 2 : 4), 256); }
 

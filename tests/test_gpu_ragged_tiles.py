@@ -58,15 +58,14 @@ def test_ffn_f32_kept_in_large_tiles():
 
 
 def test_few_rows_over_many_experts():
-    """Few rows over so many experts that the second product has more tiles than workgroups: no parts, and a workgroup takes a second tile.
-    One expert has more rows than go along with one reading of the weights."""
-    E, M, H, S, k = 92, 728, 1456, 110, 2
+    """Few rows over so many experts that the second product has more tiles than workgroups: no parts, and a workgroup takes a second tile."""
+    E, M, H, S, k = 66, 1032, 2064, 32, 2
     rng = np.random.default_rng(4)
     ns = np.ones(E, np.int64)
-    ns[7], ns[11] = 40, 0
-    ns[20:40] = 2
+    ns[[3, 4, 11, 30, 64, 65]], ns[7] = 0, 4
     n, R = int(ns.sum()), S * k
-    assert n <= R <= 8 * E and (E - 1) * -(-M // 128) > 512
+    assert n < R <= 64 and int((ns > 0).sum()) * -(-M // 128) > 512
+    assert api.moe_ragged_ffn_workspace_bytes(api.MOE_BF16, R, E, M, H, 1, 0) > 0       # of the kernels for few rows
     offsets = np.concatenate([[0], np.cumsum(ns)])
     inv = np.full(R, -1, np.int32)
     inv[:n] = rng.permutation(R)[:n]
