@@ -297,7 +297,8 @@ int moe_gate_bwd(const float* dw, const float* w, const int32_t* idx, const floa
  * The R rows are thereby a buffer of k blocks of S rows, so moe_combine_fwd / moe_combine_bwd take
  * them as they are, with E := k, C := S, idx := row_idx, slot := row_slot, inv := row_inv.
  *
- * The products read offsets on the device (clamped to 0..R and to rising order; no host copy is
+ * The products read offsets on the device (clamped to 0..R; an end in front of its beginning: no rows.
+ * Values of offsets that do not rise are unspecified, but no access leaves its tensor.  No host copy is
  * needed, calls can be captured into a graph).
  *   x    inv != NULL: token rows [S, K], row r is token inv[r] / k (inv[r] < 0 or past the last
  *        token: a row of zeros).  inv == NULL: rows [R, K] as they lie, k = 1, S ignored.
@@ -330,7 +331,7 @@ int moe_ragged_wgrad(const void* x, int dtype, int64_t S, const int32_t* inv, in
  *   forward   Z = X W1[:, h0:h0+H_l], A = GeLU(Z), Y = A W2[h0:h0+H_l, :]; A and Y use Z as computed
  *     Zq [R, H_l] int8, Zs [R, ceil(H_l/32)] uint8  out, or both NULL (nothing is kept: serving);
  *     from fp32 operands a kept Z is accumulated in fp64, because a sum next to the border between two
- *     steps decides which one is kept
+ *     steps decides which one is kept (a sum beyond fp32's range counts as an infinity)
  *     A  [R, H_l] scratch of the call, dtype;  Y [R, M] out, a partial sum when n_esp > 1
  *   backward  with z the value that (Zq, Zs) stand for, in the activation as well as in its derivative:
  *     dZ = (dY W2^T) GeLU'(z),  dX = dZ W1^T,  dW1 = X^T dZ,  dW2 = GeLU(z)^T dY
@@ -360,8 +361,8 @@ int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int64_t S, cons
  * value / step (ties to even), within +-127: off by at most half a step.
  *   q [rows, cols] int8, scales [rows, ceil(cols/32)] uint8: step = 2^(scale - 133)
  * A block with an infinity or a NaN comes back as NaN; where the doubled step would leave the range
- * (magnitudes from 0.996 * 2^128 on) the step stays 2^121 and values saturate at 127 steps; magnitudes
- * under 2^-126 have the step 2^-133.  cols % 8 == 0.
+ * (magnitudes from 0.996 * 2^128 on) the step stays 2^121 and values saturate at 127 steps; the smallest
+ * step is 2^-133, the next one takes over at 127 * 2^-133.  cols % 8 == 0.
  * --------------------------------------------------------------------------------------- */
 int moe_ckpt8_store(const void* x, int dtype, int64_t rows, int cols, void* q, void* scales,
                     void* stream);

@@ -1,10 +1,10 @@
 // 8-bit form of an activation tensor: a row is cut into blocks of 32 columns; with the largest magnitude a of a block in
 // [2^x, 2^(x+1)) its step is 2^(x - 6), or 2^(x - 5) where a / step would round to 128, and a value is kept as the whole number
-// nearest to value / step (ties to even), within +-127: an error of at most 2^-8 of the block's binade, half a step.
+// nearest to value / step (ties to even), within +-127: off by at most half a step.
 // The scale byte is b = x + 127 (+ 1 for the doubled step), so the step is 2^(b - 133).  A power of two makes both directions exact
 // but for the one rounding, and needs neither a divide nor a table.
-// Edges: blocks below 2^-126 keep the step 2^-133; a step that would need b = 255 stays 2^121 and the values saturate at 127 steps;
-// a block that holds an infinity or a NaN has b = 255 and comes back as NaN.
+// Edges: the smallest step is 2^-133, and 2^-132 takes over at 127 of them (subnormals have no binade); a step that would need
+// b = 255 stays 2^121 and the values saturate at 127 steps; a block that holds an infinity or a NaN has b = 255 and comes back as NaN.
 #pragma once
 
 #include "common.h"

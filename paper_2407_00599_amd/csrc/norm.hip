@@ -358,9 +358,14 @@ namespace {
 constexpr int MAX_M = 32768;
 constexpr int BWD_BLOCKS = 512;      // two workgroups to a compute unit
 
-// Threads to a row, and pieces to a thread (with_shape): no more than four pieces, whose weights and column sums still leave a SIMD two waves, and as few
-// threads as that allows, for what a row costs beside its bytes.  bf16, 32768 rows, the four calls: 1536 columns on 64 threads 39 / 57 / 102 / 99 us,
-// 128 39 / 55 / 88 / 78, 256 41 / 68 / 125 / 104; 1024 on 64 28 / 38 / 53 / 46, on 256 38 / 57 / 119 / 99.
+// Threads to a row, and pieces to a thread (with_shape): as few threads as leave a thread two pieces up to 4096 columns (weights, column sums and the
+// next row: two waves to a SIMD and more) and four up to 8192 (one or two; the backward kernels reach into the accumulation registers), for what a row
+// costs beside its bytes.  bf16, 32768 rows, the four calls: 1536 columns on 64 threads 39 / 57 / 102 / 99 us,
+// 128 39 / 55 / 88 / 78, 256 41 / 68 / 125 / 104; 1024 on 64 28 / 38 / 53 / 46, on 256 38 / 57 / 119 / 99; 8192 202 / 307 / 381 / 417 (5.3, 5.2, 5.6 and
+// 3.9 TB/s).
+// Wider rows take 1024 threads, which have 128 registers each.  The forward kernels fit up to 16384 columns (behind the block 328 us for 16384 rows,
+// 4.9 TB/s); behind the block from there on, and the backward kernels from 8193 columns, keep weights and sums in scratch memory and are bound by that:
+// bf16, 16384 x 16384 backward 1060 and 1133 us (2.0 and 1.4 TB/s), 8192 x 32768 behind the block 785 (2.1), backward 2388 and 2720 (0.9 and 0.6).
 int threads_per_row(int M) { return M <= 128 ? 16 : M <= 1024 ? 64 : M <= 2048 ? 128 : M <= 8192 ? 256 : 1024; }
 int groups_of(int M) { return block_of(threads_per_row(M)) / threads_per_row(M); }
 int64_t fwd_blocks(int64_t S, int M) { return std::min<int64_t>((S + groups_of(M) - 1) / groups_of(M), 2048); }

@@ -7,6 +7,8 @@
 //   forward   Z = X W1, A = GeLU(Z), Y = A W2;  Zq, Zs <- 8-bit form of Z
 //   backward  z = the value that (Zq, Zs) stand for:  A' = GeLU(z), dZ = (dY W2^T) GeLU'(z), dW2 = A'^T dY, dW1 = X^T dZ, dX = dZ W1^T
 // against the padded FFN's Z and A in the storage type, 4 bytes a value in bf16, the backward pass reads 1 + 1/32.
+// In bf16, A, A' and dZ are rounded to bf16 between two products, as the padded FFN's: they are operands of bf16 matrix instructions, and fp32 ones
+// run at a ninth of the rate.  That takes Y and the gradients from 1.66e-3 of their size off the exact ones (the last rounding alone) to 2.35e-3.
 //
 // The tiles are those of the capacity-padded calls (ffn_tile.h).  The offsets are read on the device: a workgroup finds the expert of
 // its tile by a scan over the experts' tile counts, so no count crosses to the host and a call can be captured into a graph.
@@ -413,7 +415,7 @@ void buffer_sizes(RaggedArgs& a, bool weights) {
 }
 
 // The tile of a bf16 row-tiled GEMM: the prices of the padded calls' tiles (ffn_tile.h) for what is multiplied, against the time of reading the
-// weights, 4.9 TB/s, of which a second row tile of an expert finds half in a cache.  Weights bound the launch where experts have few rows, and a tile that
+// weights, 4.9 TB/s, priced as if a second row tile of an expert found half of them in a cache.  Weights bound the launch where experts have few rows, and a tile that
 // all rows of most experts fit in is then the fastest: 8 experts of 64 rows x 4096 x 14336 and x 14336 x 4096, tiles of 128 x 128 189 and 188 us,
 // 64 x 128 198 and 243, 64 x 64 227 and 249; of 1024 x 1024 x 4096 102 and 128, 192 x 256 82.
 // wide: only tiles of eight waves.
