@@ -515,7 +515,7 @@ struct ChunkWalk {
 };
 
 // Capacity-padded rows: the layout of the calls below, as the tiles ask for it (ffn_tile.h).
-struct Padded {
+struct Padded : PlainOrder {
   using Args = GemmArgs;
   struct Place {
     int g, tm, tn;

@@ -8,6 +8,7 @@
 //   Walk       the k tiles of a weight gradient, whose reduction runs over the expert's rows
 //   store, store_f32 the epilogue
 //   map_bytes  size of the row map of a gathered operand
+//   column, k_skip, in_order   where B's columns and k indexes lie, and a map that is not there (PlainOrder)
 #pragma once
 
 #include <algorithm>
@@ -214,6 +215,15 @@ __device__ __forceinline__ int xcd_tile(const GemmArgs& p, int x, int i, int per
   return i < full ? ((i & ~31) * 8 + x * 32) + (i & 31) : full * 8 + x * (per_xcd - full) + (i - full);
 }
 
+// The order of B in memory, unless a layout says otherwise: columns and k indexes as they are numbered.
+struct PlainOrder {
+  template <int EPI>      // memory column of column c of a tile that starts at n0; one that does not exist: any that does
+  static __device__ __forceinline__ int column(const GemmArgs& p, int n0, int c) { return n0 + c < p.Ndim ? n0 + c : n0; }
+  template <int EPI>      // bytes that lie in front of k index row0 + at / 2 beside those of the k indexes before it
+  static __device__ __forceinline__ uint32_t k_skip(const GemmArgs&, int, uint32_t) { return 0u; }
+  static __device__ __forceinline__ int in_order(const GemmArgs&, int) { return 0; }     // added to entry `row` of a map
+};
+
 struct KTile {
   int row0, lim;   // first row of the k tile in the operand (row-tiled GEMMs: first k), rows (k values) that exist
 };
@@ -344,8 +354,7 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
       b_ko[j] = (uint32_t)b_k[j] * 2u;
     } else {
       b_k[j] = q * (64 / BCPR) + lane / BCPR;
-      const int col = n0 + (((lane % BCPR) ^ swz_nc(b_k[j], BCPR)) * 8);
-      b_req[j] = (uint32_t)(col < p.Ndim ? col : n0) * 2u;
+      b_req[j] = (uint32_t)L::template column<EPI>(p, n0, ((lane % BCPR) ^ swz_nc(b_k[j], BCPR)) * 8) * 2u;
       b_ko[j] = (uint32_t)b_k[j] * ldb2;
     }
   }
@@ -357,7 +366,7 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
   uint32_t g_now[RA];   // byte offset of the token row behind this lane's k-row of the next A request
   const __amdgpu_buffer_rsrc_t rG = make_rsrc(p.gather, GATHER ? L::map_bytes(p) : 0u);
   auto gather_fetch = [&](int row0) -> int {   // entries past the map read as zero; rows past the row count are masked
-    return (int)__builtin_amdgcn_raw_buffer_load_b32(rG, (row0 + lane) * 4, 0, 0);
+    return (int)__builtin_amdgcn_raw_buffer_load_b32(rG, (row0 + lane) * 4, 0, 0) + L::in_order(p, row0 + lane);
   };
   auto gather_rows = [&](int entry) -> uint64_t {   // returns which of the 64 slots are occupied
     constexpr int RPR = A_NC ? 64 / ACPR : 1;   // k-rows per request
@@ -416,7 +425,7 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
   };
   auto request_b = [&](const KTile& kt, int slot, int j) {
     const uint32_t in = b_k[j] < kt.lim ? b_ko[j] : 0u;
-    const uint32_t add = PIECES ? kb_off[PIECES ? j : 0] : (B_NC ? (uint32_t)kt.row0 * ldb2 : (uint32_t)kt.row0 * 2u) + in;
+    const uint32_t add = PIECES ? kb_off[PIECES ? j : 0] : (B_NC ? (uint32_t)kt.row0 * ldb2 : (uint32_t)kt.row0 * 2u + L::template k_skip<EPI>(p, kt.row0, in)) + in;
     dma16(rB, smem + SA * CF::A_UNIT + slot * CF::B_UNIT + (wave * RB + j) * 1024, b_req[j] + add);
   };
   auto ktile_at = [&](int t) -> KTile { return KTile{t * DK, p.Kdim - t * DK}; };   // row-tiled GEMMs
