@@ -354,6 +354,36 @@ int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int64_t S, cons
                        const int32_t* offsets, int64_t R, int E, int M, int H, int esp_idx, int n_esp,
                        void* dX, void* dW1, void* dW2, void* ws, size_t ws_bytes, void* stream);
 
+/* Gated expert FFN of one ESP shard over ragged rows.  W1 [E, M, 2 H] holds the gate's columns 0..H-1 and
+ * behind them the up projection's; the shard has columns h0..h0+H_l-1 of both halves, W2 [E, H, M] as above.
+ * act is MOE_ACT_SILU, g / (1 + exp(-g)), or MOE_ACT_GELU, the erf GeLU.
+ *   forward   G = X W1[:, h0:h0+H_l], U = X W1[:, H+h0:H+h0+H_l], A = act(G) U, Y = A W2[h0:h0+H_l, :];
+ *             A and Y use G and U as computed
+ *     Z [R, 2 H_l] out, [G | U] rounded to dtype, or NULL (nothing is kept: serving)
+ *     A [R, H_l] scratch of the call, dtype;  Y [R, M] out, a partial sum when n_esp > 1
+ *   backward  with g, u the values in Z:  dA = dY W2^T, dG = dA u act'(g), dU = dA act(g),
+ *     dX = [dG | dU] W1^T,  dW1 = X^T [dG | dU],  dW2 = (act(g) u)^T dY
+ *     dX [R, M];  dW1, dW2 FULL tensors, only the shard's columns / rows are written
+ * A dense gated FFN is E = 1 with offsets {0, R} and inv = NULL.  Rows of Z and A behind offsets[E] are not
+ * written, Y and dX hold zeros there.  Z may be brought to 8 bits between the passes (moe_ckpt8_store).
+ * fp32 accumulation, in fp32 from fp32 operands.  Workspace: backward, dG, dU, the recomputed activation and
+ * parts of the weight gradients; forward, as moe_ragged_ffn_fwd.  Limits as there, with 2 H for H and
+ * H <= 2^28. */
+enum { MOE_ACT_SILU = 0, MOE_ACT_GELU = 1 };
+
+size_t moe_ragged_glu_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp,
+                                      int backward);
+
+int moe_ragged_glu_fwd(const void* x, int dtype, int64_t S, const int32_t* inv, int k,
+                       const void* W1, const void* W2, const int32_t* offsets, int64_t R, int E,
+                       int M, int H, int esp_idx, int n_esp, int act, void* Z, void* A, void* Y,
+                       void* ws, size_t ws_bytes, void* stream);
+
+int moe_ragged_glu_bwd(const void* dY, const void* x, int dtype, int64_t S, const int32_t* inv, int k,
+                       const void* Z, const void* W1, const void* W2, const int32_t* offsets, int64_t R,
+                       int E, int M, int H, int esp_idx, int n_esp, int act, void* dX, void* dW1,
+                       void* dW2, void* ws, size_t ws_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------------
  * Activation checkpoints in 8 bits.  A row of x [rows, cols] is cut into blocks of 32 columns (the
  * last one may be short).  With a block's largest magnitude a in [2^x, 2^(x+1)) its step is 2^(x-6),

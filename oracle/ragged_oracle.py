@@ -1,5 +1,5 @@
 """Float64 checker of the dropless block's operators, written from their definitions: rows that lie expert by expert, the products over
-them, the 8-bit form of a tensor, the expert FFN whose backward pass reads that form, and the norms around the block.  It shares no code
+them, the 8-bit form of a tensor, the expert FFN whose backward pass reads that form, the norms around the block, and the gated FFN.  It shares no code
 with the HIP path."""
 import numpy as np
 from scipy.special import erf
@@ -119,3 +119,27 @@ def norm_residual_grad(dy, n, hat, rstd, w, gate, kind, alpha, layer):
     dh, dw, db = norm_grad(alpha * spread_gate(gate, kind) * dy, hat, rstd, w, layer)
     dgate = None if kind == "none" else (alpha * dy * n).sum(1 if kind == "token" else 0)
     return dh, dw, db, dgate
+
+
+def gate_act(act, g):
+    """act(g) and act'(g) of the gated FFN"""
+    if act == "gelu":
+        return gelu(g), gelu_grad(g)
+    s = 1 / (1 + np.exp(-g))
+    return g * s, s + g * s * (1 - s)
+
+
+def glu_fwd(X, Wg, Wu, W2, act, offsets):
+    """G, U, A and Y = A W2 with A = act(X Wg) X Wu"""
+    G, U = gemm(X, Wg, offsets), gemm(X, Wu, offsets)
+    A = gate_act(act, G)[0] * U
+    return G, U, A, gemm(A, W2, offsets)
+
+
+def glu_bwd(dY, X, g, u, Wg, Wu, W2, act, offsets):
+    """dG, dU, A', dX, the two halves of dW1 and dW2 at the kept g and u"""
+    a, da = gate_act(act, g)
+    dA = gemm(dY, W2.transpose(0, 2, 1), offsets)
+    dG, dU = dA * u * da, dA * a
+    dX = gemm(dG, Wg.transpose(0, 2, 1), offsets) + gemm(dU, Wu.transpose(0, 2, 1), offsets)
+    return dG, dU, a * u, dX, wgrad(X, dG, offsets), wgrad(X, dU, offsets), wgrad(a * u, dY, offsets)

@@ -17,6 +17,7 @@ MOE_F32, MOE_BF16 = 0, 1
 MOE_TILE_AUTO, MOE_TILE_SMALL, MOE_TILE_256, MOE_TILE_192 = 0, 1, 2, 3
 MOE_NORM_LAYER, MOE_NORM_RMS = 0, 1
 MOE_GATE_NONE, MOE_GATE_CHANNEL, MOE_GATE_TOKEN = 0, 1, 2
+MOE_ACT_SILU, MOE_ACT_GELU = 0, 1
 MOE_GATE_STATIC_SCRATCH_BYTES = 2 << 20
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libparm_moe.so")
@@ -106,6 +107,14 @@ def lib() -> ctypes.CDLL:
         L.moe_ragged_ffn_bwd.restype = c_i
         L.moe_ragged_ffn_bwd.argtypes = [c_p, c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_i64, c_i, c_i, c_i,
                                          c_i, c_i, c_p, c_p, c_p, c_p, c_sz, c_p]
+        L.moe_ragged_glu_workspace_bytes.restype = c_sz
+        L.moe_ragged_glu_workspace_bytes.argtypes = [c_i, c_i64, c_i, c_i, c_i, c_i, c_i]
+        L.moe_ragged_glu_fwd.restype = c_i
+        L.moe_ragged_glu_fwd.argtypes = [c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_p, c_i64, c_i, c_i, c_i, c_i, c_i, c_i,
+                                         c_p, c_p, c_p, c_p, c_sz, c_p]
+        L.moe_ragged_glu_bwd.restype = c_i
+        L.moe_ragged_glu_bwd.argtypes = [c_p, c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_p, c_p, c_i64, c_i, c_i, c_i, c_i, c_i,
+                                         c_i, c_p, c_p, c_p, c_p, c_sz, c_p]
         L.moe_ckpt8_store.restype = c_i
         L.moe_ckpt8_store.argtypes = [c_p, c_i, c_i64, c_i, c_p, c_p, c_p]
         L.moe_ckpt8_load.restype = c_i
@@ -134,6 +143,7 @@ EXPORTED = [
     "moe_choose_schedule",
     "moe_ragged_plan", "moe_ragged_gemm_workspace_bytes", "moe_ragged_gemm", "moe_ragged_wgrad_workspace_bytes",
     "moe_ragged_wgrad", "moe_ragged_ffn_workspace_bytes", "moe_ragged_ffn_fwd", "moe_ragged_ffn_bwd",
+    "moe_ragged_glu_workspace_bytes", "moe_ragged_glu_fwd", "moe_ragged_glu_bwd",
     "moe_ckpt8_store", "moe_ckpt8_load",
     "moe_norm_fwd", "moe_norm_residual_fwd", "moe_norm_bwd_workspace_bytes", "moe_norm_bwd", "moe_norm_residual_bwd",
 ]
@@ -365,6 +375,26 @@ def moe_ragged_ffn_bwd(dY, x, S, inv, k, Zq, Zs, W1, W2, offsets, R, E, M, H, es
     _check((_lib or lib()).moe_ragged_ffn_bwd(_ptr(dY), _ptr(x), _same_dtype(x, dY, W1, W2, dX, dW1, dW2), S, _ptr(inv), k,
                                               _ptr(Zq), _ptr(Zs), _ptr(W1), _ptr(W2), _ptr(offsets), R, E, M, H, esp_idx,
                                               n_esp, _ptr(dX), _ptr(dW1), _ptr(dW2), wp, wb, _stream()), "moe_ragged_ffn_bwd")
+
+
+def moe_ragged_glu_workspace_bytes(dtype, R, E, M, H, n_esp, backward) -> int:
+    return int(lib().moe_ragged_glu_workspace_bytes(dtype, R, E, M, H, n_esp, int(backward)))
+
+
+def moe_ragged_glu_fwd(x, S, inv, k, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, act, Z, A, Y, ws=None):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _check((_lib or lib()).moe_ragged_glu_fwd(_ptr(x), _same_dtype(x, W1, W2, A, Y, *([] if Z is None else [Z])), S, _ptr(inv), k, _ptr(W1),
+                                              _ptr(W2), _ptr(offsets), R, E, M, H, esp_idx, n_esp, act, _ptr(Z), _ptr(A), _ptr(Y), wp, wb,
+                                              _stream()), "moe_ragged_glu_fwd")
+
+
+def moe_ragged_glu_bwd(dY, x, S, inv, k, Z, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, act, dX, dW1, dW2, ws):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _check((_lib or lib()).moe_ragged_glu_bwd(_ptr(dY), _ptr(x), _same_dtype(x, dY, Z, W1, W2, dX, dW1, dW2), S, _ptr(inv), k, _ptr(Z),
+                                              _ptr(W1), _ptr(W2), _ptr(offsets), R, E, M, H, esp_idx, n_esp, act, _ptr(dX), _ptr(dW1),
+                                              _ptr(dW2), wp, wb, _stream()), "moe_ragged_glu_bwd")
 
 
 def moe_ckpt8_store(x, rows, cols, q, scales):

@@ -6,12 +6,16 @@
 namespace moe {
 
 enum { EPI_ACT = 16, EPI_GELU8 = 17, EPI_DGELU8 = 18 };   // GeLU alone; GeLU and the 8-bit form; dZ and GeLU from the 8-bit form
+// gated FFN (glu.hip): act(g) u alone; that and g, u; their gradients and act(g) u from g, u; a product over [dG | dU], stored
+enum { EPI_GLU = 19, EPI_GLU_KEEP = 20, EPI_DGLU = 21, EPI_GLU_DX = 22 };
 
 struct RaggedArgs : GemmArgs {     // G = E experts, Cc = R = rows of the buffers, Mdim = R in row-tiled GEMMs, C2 / Zin = the 8-bit values
   const int32_t* off;              // [E + 1]
   uint8_t* Zs;                     // [R, ldz] scales of the 8-bit values
   int ldz;
   int grid;                        // workgroups of this problem (of a part, where its reduction is split)
+  // gated FFN: columns of the gate in this shard (H / n_esp), elements from a gate column of W1 to its up column (H), the activation
+  int half, up, act;
 };
 
 struct RaggedPlace {
@@ -71,7 +75,7 @@ __device__ __forceinline__ bool find_tile(const RaggedArgs& p, int vb, RaggedPla
   for (int e0 = 0; e0 < p.G; e0 += 64) all += scan(e0);
   const int T = all * p.tiles_n, per_t = (T + 7) / 8;
   if (i >= per_t) {
-    if (EPI == EPI_STORE) fill_behind<ESZ>(p, (i - per_t) * 8 + x, p.grid - 8 * per_t);
+    if (EPI == EPI_STORE || EPI == EPI_GLU_DX) fill_behind<ESZ>(p, (i - per_t) * 8 + x, p.grid - 8 * per_t);
     return false;
   }
   const int tile = xcd_tile(p, x, i, per_t);
@@ -113,6 +117,44 @@ __device__ __forceinline__ void gelu_and_grad_fast(float z, float& g, float& dg)
   dg = fmaf(z * 0.39894228040143267794f, __builtin_amdgcn_exp2f(z * z * -0.72134752044448170368f), cdf);   // (1/2) log2(e)
 }
 
+// act(g) and act'(g) of the gated FFN, in fp32: SiLU g s with s = 1 / (1 + exp(-g)) and s (1 + g (1 - s)), or GeLU.  FAST: exp2 and the reciprocal
+// of the hardware, 1 ulp each, and the polynomial above, for values that are rounded to bf16.
+template <bool FAST>
+__device__ __forceinline__ float sigmoid(float g) {
+  if (FAST) return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.44269504088896340736f));   // log2(e)
+  return 1.0f / (1.0f + expf(-g));
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ float gate_value(float g) {
+  if (ACT == MOE_ACT_SILU) return g * sigmoid<FAST>(g);
+  return FAST ? gelu_fast(g) : gelu_f(g);
+}
+template <int ACT, bool FAST>
+__device__ __forceinline__ void gate_and_slope(float g, float& a, float& da) {
+  if (ACT == MOE_ACT_SILU) {
+    const float s = sigmoid<FAST>(g);
+    a = g * s;
+    da = fmaf(a, 1.0f - s, s);
+  } else if (FAST) {
+    gelu_and_grad_fast(g, a, da);
+  } else {
+    gelu_and_grad(g, a, da);
+  }
+}
+// f(integral_constant<int, ACT>) for the activation of a call
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F&& f) {
+  if (act == MOE_ACT_SILU) f(std::integral_constant<int, MOE_ACT_SILU>{});
+  else f(std::integral_constant<int, MOE_ACT_GELU>{});
+}
+// hidden column of column c of a gated first product's tile, whose pieces of 32 columns are 16 of the gate and the same 16 of the up projection
+__device__ __forceinline__ int glu_hidden(int c) { return (c >> 5) * 16 + (c & 15); }
+// its column in W1 (of the shard), or one that exists
+__device__ __forceinline__ int glu_column(const RaggedArgs& p, int n0, int c) {
+  const int h = glu_hidden(n0 + c);
+  return h < p.half ? h + ((c & 16) ? p.up : 0) : 0;
+}
+
 // The FFN of few rows (ragged_few.hip): bf16, nothing kept for a backward pass; ws of few_rows_bytes().
 size_t few_rows_bytes(int64_t R, int E, int M, int Hl);
 void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, void* ws, hipStream_t st);
@@ -122,6 +164,12 @@ constexpr int F32_TILE = 64, KC = 32;      // tile, k chunk
 template <int KIND, int EPI>
 void launch_f32(RaggedArgs a, hipStream_t st);
 void launch_trio_f32(RaggedArgs dx, RaggedArgs w2, RaggedArgs w1, hipStream_t st);
+void launch_glu_bwd_f32(RaggedArgs dx, RaggedArgs w2, RaggedArgs wg, RaggedArgs wu, hipStream_t st);
+
+// the FFN's second product with a reduction in parts where that pays and ws has room for them, and the sums of one or two split weight
+// gradients of the same size (ragged.hip)
+void launch_second(const RaggedArgs& y, int dtype, void* ws, size_t ws_bytes, hipStream_t st);
+void add_parts(const RaggedArgs& p2, const RaggedArgs& p1, int problems, int dtype, hipStream_t st);
 
 // ---- host side ----
 // Row tiles that R rows of E experts are priced at: half a tile of each expert's last one is empty.  How the rows are spread is not

@@ -156,13 +156,6 @@ void launch_rows(RaggedArgs a, int dtype, hipStream_t st) {
 }
 
 
-void add_parts(const RaggedArgs& p2, const RaggedArgs& p1, int problems, int dtype, hipStream_t st) {
-  const int64_t n = (int64_t)p2.G * p2.Mdim * p2.Ndim / 4;       // sizes are multiples of 8
-  const dim3 grid((unsigned)((problems * n + 255) / 256));
-  if (dtype == MOE_BF16) hipLaunchKernelGGL((ragged_add_parts<bf16_t>), grid, dim3(256), 0, st, p2, p1, n, problems * n);
-  else hipLaunchKernelGGL((ragged_add_parts<float>), grid, dim3(256), 0, st, p2, p1, n, problems * n);
-}
-
 // one weight gradient; parts: room for a.splits of them
 void launch_weights(RaggedArgs a, int dtype, float* parts, hipStream_t st) {
   a.part = parts;
@@ -235,6 +228,20 @@ bool few_rows(int dtype, int64_t R, int E, int M, int Hl) {
 }
 
 }  // namespace
+
+void launch_second(const RaggedArgs& y, int dtype, void* ws, size_t ws_bytes, hipStream_t st) {
+  const int parts = row_parts(dtype, y.R, y.G, y.Kdim, y.Ndim);
+  if (parts > 1 && ws != nullptr && ws_bytes >= row_part_bytes(parts, y.R, y.Ndim)) launch_row_parts<KIND_NN>(y, parts, ws, st);
+  else launch_rows<KIND_NN, EPI_STORE>(y, dtype, st);
+}
+
+void add_parts(const RaggedArgs& p2, const RaggedArgs& p1, int problems, int dtype, hipStream_t st) {
+  const int64_t n = (int64_t)p2.G * p2.Mdim * p2.Ndim / 4;       // sizes are multiples of 8
+  const dim3 grid((unsigned)((problems * n + 255) / 256));
+  if (dtype == MOE_BF16) hipLaunchKernelGGL((ragged_add_parts<bf16_t>), grid, dim3(256), 0, st, p2, p1, n, problems * n);
+  else hipLaunchKernelGGL((ragged_add_parts<float>), grid, dim3(256), 0, st, p2, p1, n, problems * n);
+}
+
 }  // namespace moe
 
 using namespace moe;
@@ -339,9 +346,7 @@ extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int
   }
   if (Zq) launch_rows<KIND_NN, EPI_GELU8>(a, dtype, st);
   else launch_rows<KIND_NN, EPI_ACT>(a, dtype, st);
-  const int parts = row_parts(dtype, R, E, Hl, M);
-  if (parts > 1 && ws != nullptr && ws_bytes >= row_part_bytes(parts, R, M)) launch_row_parts<KIND_NN>(y, parts, ws, st);
-  else launch_rows<KIND_NN, EPI_STORE>(y, dtype, st);
+  launch_second(y, dtype, ws, ws_bytes, st);
   return check_launch();
 }
 

@@ -41,9 +41,48 @@ struct Operand {       // one operand of a tile in LDS, and a thread's part in b
 template <int KIND, int T>
 constexpr int f32_floats() { return 2 * (Operand<T, KIND == KIND_TN>::FLOATS + Operand<T, KIND != KIND_NT>::FLOATS); }
 
+// Epilogues of the gated FFN.  Forward: 16 lanes hold g of a row and the 16 next to them its u.
+template <int EPI, int T, int ACT>
+__device__ __forceinline__ void store_glu(const RaggedArgs& p, const f32x16_t (&total)[T / 64][T / 64], const RaggedPlace& at, int m0, int n0,
+                                          int wm, int wn, int lane) {
+  constexpr int W = T / 2, NB = W / 32;
+  const int l32 = lane & 31, half = lane >> 5;
+  float* __restrict__ A = reinterpret_cast<float*>(p.C);      // act(g) u
+  float* __restrict__ Z = reinterpret_cast<float*>(p.C2);     // [g | u], or their gradients
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int m = m0 + wm * W + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
+      const int64_t row = at.lo + m;
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const float v = total[i][j][r];
+        const int c = n0 + wn * W + 32 * j + l32;
+        if constexpr (EPI == EPI_DGLU) {
+          if (m >= at.n || c >= p.half) continue;
+          const float* __restrict__ z = reinterpret_cast<const float*>(p.Zin) + row * 2 * p.half + c;
+          const float u = z[p.half];
+          float a, da;
+          gate_and_slope<ACT, false>(z[0], a, da);
+          A[row * p.half + c] = a * u;
+          Z[row * 2 * p.half + c] = v * u * da;
+          Z[row * 2 * p.half + p.half + c] = v * a;
+        } else {
+          const float w = __shfl_xor(v, 16, 64);
+          const int h = glu_hidden(c);
+          if (m >= at.n || h >= p.half) continue;
+          if (l32 < 16) A[row * p.half + h] = gate_value<ACT, false>(v) * w;
+          if (EPI == EPI_GLU_KEEP) Z[row * 2 * p.half + (l32 < 16 ? h : p.half + h)] = v;
+        }
+      }
+    }
+}
+
 template <int KIND, int EPI, int T>
 __device__ __forceinline__ void f32_tile(const RaggedArgs& p, float* smem, int vb) {
   constexpr bool A_SLOW = KIND == KIND_TN, B_SLOW = KIND != KIND_NT;
+  constexpr bool GLU = EPI == EPI_GLU || EPI == EPI_GLU_KEEP;
   using OA = Operand<T, A_SLOW>;
   using OB = Operand<T, B_SLOW>;
   constexpr int UA = OA::U, UB = OB::U, W = T / 2, NB = W / 32;
@@ -91,8 +130,9 @@ __device__ __forceinline__ void f32_tile(const RaggedArgs& p, float* smem, int v
 #pragma unroll
   for (int u = 0; u < UB; ++u) {
     const int c = OB::at_of(tid, u);
-    okb[u] = n0 + c < p.Ndim;
-    pb[u] = B + (B_SLOW ? (int64_t)(okb[u] ? n0 + c : 0) : (int64_t)(okb[u] ? n0 + c : 0) * p.ldb);
+    okb[u] = GLU ? glu_hidden(n0 + c) < p.half : n0 + c < p.Ndim;
+    if (GLU) pb[u] = B + glu_column(p, n0, c);
+    else pb[u] = B + (B_SLOW ? (int64_t)(okb[u] ? n0 + c : 0) : (int64_t)(okb[u] ? n0 + c : 0) * p.ldb);
   }
   // token rows of a reduction: map entries of the chunk that is requested next
   int entry[A_SLOW ? UA : 1];
@@ -132,7 +172,7 @@ __device__ __forceinline__ void f32_tile(const RaggedArgs& p, float* smem, int v
 #pragma unroll
     for (int u = 0; u < UB; ++u) {
       const int k = c * KC + OB::k_of(tid, u), kk = k < K ? k : 0;
-      const int64_t off = KIND == KIND_TN ? (int64_t)(at.lo + kk) * p.ldb : B_SLOW ? (int64_t)kk * p.ldb : kk;
+      const int64_t off = KIND == KIND_TN ? (int64_t)(at.lo + kk) * p.ldb : B_SLOW ? (int64_t)kk * p.ldb : kk + (EPI == EPI_GLU_DX && kk >= p.half ? p.up - p.half : 0);
       d.b[u] = *reinterpret_cast<const f32x4_t*>(pb[u] + off);
       d.keep_b |= (uint32_t)(okb[u] && k < K) << u;
     }
@@ -219,6 +259,10 @@ __device__ __forceinline__ void f32_tile(const RaggedArgs& p, float* smem, int v
     flush();
   }
 
+  if constexpr (GLU || EPI == EPI_DGLU) {
+    with_act(p.act, [&](auto act) { store_glu<EPI, T, decltype(act)::value>(p, total, at, m0, n0, wm, wn, lane); });
+    return;
+  }
   float* __restrict__ C = EPI == EPI_PART ? p.part : reinterpret_cast<float*>(p.C);
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -238,11 +282,11 @@ __device__ __forceinline__ void f32_tile(const RaggedArgs& p, float* smem, int v
         const int n = n0 + wn * W + 32 * j + l32;
         if (n >= p.Ndim) continue;
         const float v = total[i][j][r];
-        if constexpr (EPI == EPI_STORE || EPI == EPI_PART) {
+        if constexpr (EPI == EPI_STORE || EPI == EPI_PART || EPI == EPI_GLU_DX) {
           C[row + n] = v;
         } else if constexpr (EPI == EPI_ACT) {
           C[row + n] = gelu_f(v);
-        } else {
+        } else if constexpr (EPI == EPI_DGELU8) {
           float ge, dg;
           const uint32_t q = reinterpret_cast<const uint8_t*>(p.Zin)[row + n];
           gelu_and_grad(ckpt8_value(q, 0, p.Zs[(int64_t)(at.lo + m) * p.ldz + (n >> 5)]), ge, dg);
@@ -268,6 +312,16 @@ __global__ __launch_bounds__(256, 2) void ragged_bwd_trio_f32(const RaggedArgs p
   else f32_tile<KIND_TN, EPI, F32_TILE>(b < nbx + nb2 ? pw2 : pw1, smem, b < nbx + nb2 ? b - nbx : b - nbx - nb2);
 }
 
+// the four of the gated FFN: dX over [dG | dU], dW2, and the gate's and the up projection's half of dW1
+template <int EPI>
+__global__ __launch_bounds__(256, 2) void ragged_glu_bwd_f32(const RaggedArgs px, const RaggedArgs pw2, const RaggedArgs pwg, const RaggedArgs pwu,
+                                                             int nbx, int nbw) {
+  __shared__ __attribute__((aligned(16))) float smem[f32_floats<KIND_TN, F32_TILE>()];
+  const int b = (int)blockIdx.x;
+  if (b < nbx) f32_tile<KIND_NT, EPI_GLU_DX, F32_TILE>(px, smem, b);
+  else f32_tile<KIND_TN, EPI, F32_TILE>(b < nbx + nbw ? pw2 : b < nbx + 2 * nbw ? pwg : pwu, smem, (b - nbx) % nbw);
+}
+
 template <int KIND, int EPI>
 void launch_f32(RaggedArgs a, hipStream_t st) {
   const dim3 grid = KIND == KIND_TN ? size_weights(a, F32_TILE) : size_rows(a, F32_TILE, F32_TILE, EPI == EPI_STORE);
@@ -279,6 +333,9 @@ template void launch_f32<KIND_NN, EPI_ACT>(RaggedArgs, hipStream_t);
 template void launch_f32<KIND_NT, EPI_STORE>(RaggedArgs, hipStream_t);
 template void launch_f32<KIND_NT, EPI_PART>(RaggedArgs, hipStream_t);
 template void launch_f32<KIND_NT, EPI_DGELU8>(RaggedArgs, hipStream_t);
+template void launch_f32<KIND_NN, EPI_GLU>(RaggedArgs, hipStream_t);
+template void launch_f32<KIND_NN, EPI_GLU_KEEP>(RaggedArgs, hipStream_t);
+template void launch_f32<KIND_NT, EPI_DGLU>(RaggedArgs, hipStream_t);
 template void launch_f32<KIND_TN, EPI_STORE>(RaggedArgs, hipStream_t);
 template void launch_f32<KIND_TN, EPI_PART>(RaggedArgs, hipStream_t);
 
@@ -288,6 +345,16 @@ void launch_trio_f32(RaggedArgs dx, RaggedArgs w2, RaggedArgs w1, hipStream_t st
   const dim3 grid(nbx + nb2 + nb1);
   if (w2.splits > 1) hipLaunchKernelGGL((ragged_bwd_trio_f32<EPI_PART>), grid, dim3(256), 0, st, dx, w2, w1, (int)nbx, (int)nb2);
   else hipLaunchKernelGGL((ragged_bwd_trio_f32<EPI_STORE>), grid, dim3(256), 0, st, dx, w2, w1, (int)nbx, (int)nb2);
+}
+
+void launch_glu_bwd_f32(RaggedArgs dx, RaggedArgs w2, RaggedArgs wg, RaggedArgs wu, hipStream_t st) {
+  const unsigned nbx = size_rows(dx, F32_TILE, F32_TILE, true).x;
+  const unsigned nbw = size_weights(w2, F32_TILE).x * w2.splits;       // the three have as many tiles each
+  size_weights(wg, F32_TILE);
+  size_weights(wu, F32_TILE);
+  const dim3 grid(nbx + 3 * nbw);
+  if (w2.splits > 1) hipLaunchKernelGGL((ragged_glu_bwd_f32<EPI_PART>), grid, dim3(256), 0, st, dx, w2, wg, wu, (int)nbx, (int)nbw);
+  else hipLaunchKernelGGL((ragged_glu_bwd_f32<EPI_STORE>), grid, dim3(256), 0, st, dx, w2, wg, wu, (int)nbx, (int)nbw);
 }
 
 }  // namespace moe
