@@ -400,6 +400,49 @@ int moe_ckpt8_load(const void* q, const void* scales, int64_t rows, int cols, vo
                    void* stream);
 
 /* ---------------------------------------------------------------------------------------
+ * Microscaled 4-bit floating point.  Along the index that a product sums over, values are cut into blocks of
+ * 32 (the last one may be short).  With a block's largest magnitude a in [2^x, 2^(x+1)) its scale is 2^(x-2),
+ * twice that where a / scale would round to 8; a value is kept as the one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 and
+ * their negatives (codes 0..7, and 8 more for the sign) that is nearest to value / scale, of two the one
+ * with the even code.  The scale byte b stands for 2^(b-127); 0 is the smallest, 252 the largest (magnitudes
+ * from 1.75 * 2^127 on become 1.5 * 2^127), 255 is NaN, for a block that holds an infinity or a NaN.  A matrix with n rows of K summed values is held as
+ *   q      [n, ceil(K/32), 16] bytes, two values each, the even index in the low half, zeros behind the K-th
+ *   scales [ceil(K/512), 4, n, 4] bytes, block 16 c + 4 s + p of row r at [c, p, r, s] (what lies behind
+ *          the last block is written as zero and may hold anything where it is read)
+ *   moe_mx4_store   x [G, rows, cols] -> G matrices; transposed = 0: n = rows, K = cols (activations);
+ *                   transposed = 1: n = cols, K = rows (expert weights [E, K, N], which are summed over K)
+ *   moe_mx4_load    back to x [G, rows, cols]
+ * cols % 8 == 0, transposed also rows % 8 == 0.
+ *
+ * moe_ragged_gemm_mx4: Y [R, N] = X W of each row's expert, rows and offsets as in moe_ragged_gemm;
+ *   xq, xs  the token matrix (S rows of K; inv == NULL: R rows);  Wq, Ws  the experts' [E, K, N], stored with
+ *   transposed = 1;  Y of `dtype`, rows behind offsets[E] are zeros.  Products are exact, sums fp32.
+ * moe_ragged_glu_mx4: the gated FFN served from 4 bits.  x [S, M] (inv == NULL: [R, M]) of `dtype` is brought to
+ *   4 bits row by row, G and U are its products with W1 [E, M, 2 H], A = act(G) U is brought to 4 bits row by row,
+ *   Y [R, M] (dtype) = A W2, W2 [E, H, M]; both stored with transposed = 1.  A rank with a hidden shard stores
+ *   its own columns / rows (H is then its share, Y a partial sum).  Workspace: x and A in 4 bits.
+ * Limits: E <= 256, K, N, M, H multiples of 8, S*k and R at most 2^29, the 4-bit values of X, of A and of one
+ * expert's matrix under 4 GiB each.
+ * --------------------------------------------------------------------------------------- */
+int moe_mx4_store(const void* x, int dtype, int64_t G, int64_t rows, int cols, int transposed, void* q,
+                  void* scales, void* stream);
+
+int moe_mx4_load(const void* q, const void* scales, int64_t G, int64_t rows, int cols, int transposed,
+                 void* x, int dtype, void* stream);
+
+size_t moe_ragged_gemm_mx4_workspace_bytes(int64_t R, int E, int K, int N);
+
+int moe_ragged_gemm_mx4(const void* xq, const void* xs, int64_t S, const int32_t* inv, int k,
+                        const void* Wq, const void* Ws, const int32_t* offsets, int64_t R, int E, int K,
+                        int N, void* Y, int dtype, void* ws, size_t ws_bytes, void* stream);
+
+size_t moe_ragged_glu_mx4_workspace_bytes(int64_t S, int64_t R, int E, int M, int H);
+
+int moe_ragged_glu_mx4(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* W1q,
+                       const void* W1s, const void* W2q, const void* W2s, const int32_t* offsets, int64_t R,
+                       int E, int M, int H, int act, void* Y, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------
  * Norms in front of and behind a block, over rows [S, M] of `dtype`; w, b, gate, the statistics and all
  * weight gradients are fp32, statistics and sums are formed in fp32.
  *   MOE_NORM_LAYER  n(v) = (v - mean) / sqrt(var + eps) * w + b   (b NULL: none)

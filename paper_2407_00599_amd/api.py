@@ -119,6 +119,19 @@ def lib() -> ctypes.CDLL:
         L.moe_ckpt8_store.argtypes = [c_p, c_i, c_i64, c_i, c_p, c_p, c_p]
         L.moe_ckpt8_load.restype = c_i
         L.moe_ckpt8_load.argtypes = [c_p, c_p, c_i64, c_i, c_p, c_i, c_p]
+        L.moe_mx4_store.restype = c_i
+        L.moe_mx4_store.argtypes = [c_p, c_i, c_i64, c_i64, c_i, c_i, c_p, c_p, c_p]
+        L.moe_mx4_load.restype = c_i
+        L.moe_mx4_load.argtypes = [c_p, c_p, c_i64, c_i64, c_i, c_i, c_p, c_i, c_p]
+        L.moe_ragged_gemm_mx4_workspace_bytes.restype = c_sz
+        L.moe_ragged_gemm_mx4_workspace_bytes.argtypes = [c_i64, c_i, c_i, c_i]
+        L.moe_ragged_gemm_mx4.restype = c_i
+        L.moe_ragged_gemm_mx4.argtypes = [c_p, c_p, c_i64, c_p, c_i, c_p, c_p, c_p, c_i64, c_i, c_i, c_i, c_p, c_i, c_p, c_sz, c_p]
+        L.moe_ragged_glu_mx4_workspace_bytes.restype = c_sz
+        L.moe_ragged_glu_mx4_workspace_bytes.argtypes = [c_i64, c_i64, c_i, c_i, c_i]
+        L.moe_ragged_glu_mx4.restype = c_i
+        L.moe_ragged_glu_mx4.argtypes = [c_p, c_i, c_i64, c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_i64, c_i, c_i, c_i, c_i, c_p, c_p, c_sz,
+                                         c_p]
         L.moe_norm_fwd.restype = c_i
         L.moe_norm_fwd.argtypes = [c_p, c_i, c_i64, c_i, c_i, c_p, c_p, c_f, c_p, c_p, c_p, c_p]
         L.moe_norm_residual_fwd.restype = c_i
@@ -145,6 +158,8 @@ EXPORTED = [
     "moe_ragged_wgrad", "moe_ragged_ffn_workspace_bytes", "moe_ragged_ffn_fwd", "moe_ragged_ffn_bwd",
     "moe_ragged_glu_workspace_bytes", "moe_ragged_glu_fwd", "moe_ragged_glu_bwd",
     "moe_ckpt8_store", "moe_ckpt8_load",
+    "moe_mx4_store", "moe_mx4_load", "moe_ragged_gemm_mx4_workspace_bytes", "moe_ragged_gemm_mx4",
+    "moe_ragged_glu_mx4_workspace_bytes", "moe_ragged_glu_mx4",
     "moe_norm_fwd", "moe_norm_residual_fwd", "moe_norm_bwd_workspace_bytes", "moe_norm_bwd", "moe_norm_residual_bwd",
 ]
 
@@ -409,6 +424,48 @@ def moe_ckpt8_load(q, scales, rows, cols, x):
     _typed(torch.uint8, scales)
     _check((_lib or lib()).moe_ckpt8_load(_ptr(q), _ptr(scales), rows, cols, _ptr(x), dtype_code(x), _stream()),
            "moe_ckpt8_load")
+
+
+def mx4_shapes(G, rows, cols, transposed):
+    """Shapes of the bytes that moe_mx4_store writes: values, scales."""
+    n, K = (cols, rows) if transposed else (rows, cols)
+    return (G, n, (K + 31) // 32 * 16), (G, (K + 511) // 512, 4, n, 4)
+
+
+def moe_mx4_store(x, G, rows, cols, transposed, q, scales):
+    _typed(torch.uint8, q, scales)
+    _check((_lib or lib()).moe_mx4_store(_ptr(x), dtype_code(x), G, rows, cols, int(transposed), _ptr(q), _ptr(scales), _stream()),
+           "moe_mx4_store")
+
+
+def moe_mx4_load(q, scales, G, rows, cols, transposed, x):
+    _typed(torch.uint8, q, scales)
+    _check((_lib or lib()).moe_mx4_load(_ptr(q), _ptr(scales), G, rows, cols, int(transposed), _ptr(x), dtype_code(x), _stream()),
+           "moe_mx4_load")
+
+
+def moe_ragged_gemm_mx4_workspace_bytes(R, E, K, N) -> int:
+    return int(lib().moe_ragged_gemm_mx4_workspace_bytes(R, E, K, N))
+
+
+def moe_ragged_gemm_mx4(xq, xs, S, inv, k, Wq, Ws, offsets, R, E, K, N, Y, ws=None):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _typed(torch.uint8, xq, xs, Wq, Ws)
+    _check((_lib or lib()).moe_ragged_gemm_mx4(_ptr(xq), _ptr(xs), S, _ptr(inv), k, _ptr(Wq), _ptr(Ws), _ptr(offsets), R, E, K, N, _ptr(Y),
+                                               dtype_code(Y), wp, wb, _stream()), "moe_ragged_gemm_mx4")
+
+
+def moe_ragged_glu_mx4_workspace_bytes(S, R, E, M, H) -> int:
+    return int(lib().moe_ragged_glu_mx4_workspace_bytes(S, R, E, M, H))
+
+
+def moe_ragged_glu_mx4(x, S, inv, k, W1q, W1s, W2q, W2s, offsets, R, E, M, H, act, Y, ws):
+    wp, wb = _ws_args(ws)
+    _typed(torch.int32, inv, offsets)
+    _typed(torch.uint8, W1q, W1s, W2q, W2s)
+    _check((_lib or lib()).moe_ragged_glu_mx4(_ptr(x), _same_dtype(x, Y), S, _ptr(inv), k, _ptr(W1q), _ptr(W1s), _ptr(W2q), _ptr(W2s),
+                                              _ptr(offsets), R, E, M, H, act, _ptr(Y), wp, wb, _stream()), "moe_ragged_glu_mx4")
 
 
 def moe_norm_fwd(x, S, M, kind, w, b, eps, u, mean=None, rstd=None):

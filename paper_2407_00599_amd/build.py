@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libparm_moe.so")
 SOURCES = ["api.hip", "gate.hip", "permute.hip", "ffn.hip", "gate_bwd.hip", "schedule.hip", "ragged.hip",
-           "ragged_few.hip", "ragged_f32.hip", "glu.hip", "ckpt8.hip", "norm.hip"]
+           "ragged_few.hip", "ragged_f32.hip", "glu.hip", "mx4.hip", "mx4_few.hip", "mx4_ffn.hip", "ckpt8.hip", "norm.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-fvisibility=default",

@@ -1,0 +1,215 @@
+"""GPU parity of microscaled 4-bit floating point against the float64 checker: the bytes bit for bit, products and the gated FFN served from them
+element by element.
+
+Bounds.  Products of two 4-bit values are exact; a sum of K of them carries at most K 2^-23 of the sum of magnitudes in fp32, as in test_gpu_ragged.py.  Of
+the FFN's hidden values, which are known to some bound, 4 bits keep anything between what the ends of that range are kept as (O.kept_range); beyond
+that its second product is one of exact values."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as O
+from oracle import ragged_oracle as RO
+from paper_2407_00599_amd import api
+from test_gpu_glu import CODE, act_bounds
+from test_gpu_ragged import Case, check, host
+from util import DEV, torch_dtype
+
+pytestmark = pytest.mark.gpu
+
+
+def store(x, transposed):
+    """x [G, rows, cols] on the GPU -> bytes"""
+    G, rows, cols = x.shape
+    q, s = (torch.full(shape, 0x5A, dtype=torch.uint8, device=DEV) for shape in api.mx4_shapes(G, rows, cols, transposed))
+    api.moe_mx4_store(x, G, rows, cols, transposed, q, s)
+    return q, s
+
+
+def tensor(rng, G, rows, cols, dtype):
+    """Magnitudes of many binades, blocks of zeros, ties between two codes, the border of the doubled scale, values that bf16 and fp32 hold exactly."""
+    x = rng.standard_normal((G, rows, cols)) * np.exp2(rng.integers(-30, 30, (G, rows, 1)))
+    x[:, ::5] = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 0.0, -0.0, -0.25, -7.0], (G, len(range(0, rows, 5)), cols))
+    x[:, 1::7] = 0
+    return torch.from_numpy(x).to(torch_dtype(dtype)).to(DEV)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("G,rows,cols", [(1, 1, 8), (1, 8, 8), (2, 3, 40), (1, 5, 32), (3, 70, 128), (1, 33, 136), (2, 66, 256), (1, 17, 264), (1, 67, 520),
+                                         (1, 9, 1544), (2, 512, 24), (1, 520, 264), (1, 1032, 8), (1, 64, 2048)])
+@pytest.mark.parametrize("transposed", [False, True])
+def test_bytes_and_back(G, rows, cols, transposed, dtype):
+    if transposed:
+        rows = -(-rows // 8) * 8
+    x = tensor(np.random.default_rng(rows + cols), G, rows, cols, dtype)
+    q, s = store(x, transposed)
+    back = torch.full_like(x, 7)
+    api.moe_mx4_load(q, s, G, rows, cols, transposed, back)
+    for g in range(G):
+        v = host(x[g]).T if transposed else host(x[g])
+        codes, scales = O.store(v)
+        rq, rs = O.pack(codes, scales)
+        assert np.array_equal(host(s[g]), rs) and np.array_equal(host(q[g]), rq)
+        ref = O.values(codes, scales)[:, :v.shape[1]]
+        assert np.array_equal(host(back[g]), ref.T if transposed else ref)
+
+
+@pytest.mark.parametrize("transposed", [False, True])
+def test_edges_of_the_range(transposed):
+    """The smallest and largest magnitudes; an infinity or a NaN takes its block, not its neighbours."""
+    x = np.zeros((1, 64, 64), np.float32)
+    x[0, 0, :32] = 2.0 ** -149 * np.arange(32)
+    x[0, 1, :32] = np.float32(2.0 ** -127) * np.arange(32) / 4
+    x[0, 2, :32] = np.float32(3.4e38) * (np.arange(32) - 16) / 16
+    x[0, 3, 5], x[0, 4, 40], x[0, 5, 31] = np.inf, np.nan, -np.inf
+    x[0, 3:6] += 1
+    if transposed:
+        x = x.transpose(0, 2, 1).copy()
+    t = torch.from_numpy(x).to(DEV)
+    q, s = store(t, transposed)
+    v = x[0].T if transposed else x[0]
+    codes, scales = O.store(v)
+    rq, rs = O.pack(codes, scales)
+    assert np.array_equal(host(s[0]), rs) and np.array_equal(host(q[0]), rq)
+    back = torch.empty_like(t)
+    api.moe_mx4_load(q, s, 1, 64, 64, transposed, back)
+    got, ref = host(back[0]), O.values(codes, scales)
+    assert np.array_equal(np.isnan(got.T if transposed else got), np.isnan(ref)) and np.isnan(ref).sum() == 96
+    assert np.array_equal(np.nan_to_num(got.T if transposed else got), np.nan_to_num(ref))
+
+
+class Four:
+    """A Case's rows in 4 bits, and experts' weights"""
+
+    def __init__(self, ns, behind, K, dtype, gather):
+        c = self.c = Case(ns, behind, K, 0, dtype, gather, 5 * K + sum(ns))
+        rows = c.S if gather else c.R
+        c.x[::3] *= 16
+        self.xq, self.xs = store(c.x.view(1, rows, K), False)
+        kept = O.kept(host(c.x))
+        self.X = RO.rows_of(kept, host(c.inv), c.k) if gather else kept.copy()
+        self.rows = rows
+
+    def weights(self, K, N, gain=1.0):
+        """bytes and what they stand for, [E, K, N]"""
+        W = self.c.stored(self.c.rng.standard_normal((self.c.E, K, N)) * gain / np.sqrt(K))
+        q, s = store(W, True)
+        return q, s, np.stack([O.kept(host(w).T).T for w in W])
+
+
+# rows per expert, rows behind, K, N, gather
+PRODUCTS = [
+    ((1,), 0, 8, 8, True), ((1, 0), 1, 64, 128, True), ((0, 0, 3), 2, 72, 40, False), ((0,), 9, 64, 64, False), ((5, 0, 17, 64, 1), 4, 264, 136, True),
+    ((33, 31, 32, 64, 65), 0, 128, 256, True), ((200, 0, 55), 70, 520, 328, True), ((1,) * 70 + (0,) * 10 + (4,) * 20, 3, 64, 72, True),
+    ((300, 513), 1, 1032, 72, False), ((3, 1), 0, 2056, 264, True), ((20,), 5, 4096, 64, True), ((2,) * 8, 0, 1024, 512, True),
+    ((700, 0, 90), 20, 520, 520, True), ((1300, 257), 0, 264, 776, False),
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("ns,behind,K,N,gather", PRODUCTS)
+def test_products(ns, behind, K, N, gather, dtype):
+    f = Four(ns, behind, K, dtype, gather)
+    c = f.c
+    Wq, Ws, W = f.weights(K, N)
+    ws = torch.empty(api.moe_ragged_gemm_mx4_workspace_bytes(c.R, c.E, K, N) + 16, dtype=torch.uint8, device=DEV)
+    Y = c.fresh(c.R, N)
+    api.moe_ragged_gemm_mx4(f.xq, f.xs, c.S, c.inv, c.k, Wq, Ws, c.off, c.R, c.E, K, N, Y, ws)
+    ref = RO.gemm(f.X, W, c.offsets)
+    check(Y, ref, c.half * np.abs(ref) + (1 + c.half) * c.sums(K) * RO.gemm(np.abs(f.X), np.abs(W), c.offsets), "Y")
+
+
+# rows per expert, rows behind, M, H, gather
+GLU = [
+    ((1,), 0, 8, 8, True), ((1,), 0, 64, 64, False), ((2, 0, 1), 1, 64, 128, True), ((0, 0), 3, 64, 64, True), ((20, 0, 45, 9), 6, 136, 272, True),
+    ((64, 33, 0, 100), 0, 72, 1032, False), ((150, 70), 40, 264, 520, True), ((3,) * 66, 0, 64, 40, True), ((400, 90, 313), 30, 128, 200, True),
+    ((0, 3, 0, 0, 1, 0, 7, 0), 3, 520, 2200, True), ((700, 0, 90), 10, 72, 264, True),
+]
+
+
+@pytest.mark.parametrize("dtype,act", [("f32", "silu"), ("bf16", "silu"), ("bf16", "gelu")])
+@pytest.mark.parametrize("ns,behind,M,H,gather", GLU)
+def test_glu(ns, behind, M, H, gather, dtype, act):
+    f = Four(ns, behind, M, dtype, gather)
+    c, off = f.c, f.c.offsets
+    W1q, W1s, W1 = f.weights(M, 2 * H)
+    W2q, W2s, W2 = f.weights(H, M)
+    wg, wu = W1[:, :, :H], W1[:, :, H:]
+    ws = torch.empty(api.moe_ragged_glu_mx4_workspace_bytes(c.S, c.R, c.E, M, H), dtype=torch.uint8, device=DEV)
+    ws.fill_(255)                                   # scales that nothing writes are those of NaN
+    Y = c.fresh(c.R, M)
+    api.moe_ragged_glu_mx4(c.x, c.S, c.inv, c.k, W1q, W1s, W2q, W2s, c.off, c.R, c.E, M, H, CODE[act], Y, ws)
+    X = np.abs(f.X)
+    G, U = RO.gemm(f.X, wg, off), RO.gemm(f.X, wu, off)
+    dG, dU = c.sums(M) * RO.gemm(X, np.abs(wg), off), c.sums(M) * RO.gemm(X, np.abs(wu), off)
+    a = O.glu(f.X, wg, wu, act, off)
+    ea = act_bounds(act, "f32", np.abs(G) + dG)[0] + 1.13 * dG
+    d = ea * (np.abs(U) + dU) + np.abs(RO.gate_act(act, G)[0]) * dU + 2.0 ** -23 * np.abs(a)
+    lo, hi = O.kept_range(a, d)
+    kept = O.kept(a)
+    spread = np.maximum(hi - kept, kept - lo)
+    ref = RO.gemm(kept, W2, off)
+    b = RO.gemm(spread, np.abs(W2), off) + c.sums(H) * RO.gemm(np.abs(kept) + spread, np.abs(W2), off)
+    check(Y, ref, b + c.half * (np.abs(ref) + b), "Y")
+
+
+def test_scales_behind_the_last_block_may_hold_anything():
+    f = Four((9, 30), 2, 136, "f32", True)          # five blocks
+    c = f.c
+    Wq, Ws, W = f.weights(136, 72)
+    f.xs[:, :, 1:, :, 1:], Ws[:, :, 1:, :, 1:], f.xs[..., 2:], Ws[..., 2:] = 255, 255, 255, 255
+    Y = c.fresh(c.R, 72)
+    api.moe_ragged_gemm_mx4(f.xq, f.xs, c.S, c.inv, c.k, Wq, Ws, c.off, c.R, c.E, 136, 72, Y)
+    ref = RO.gemm(f.X, W, c.offsets)
+    check(Y, ref, 2 * c.sums(136) * RO.gemm(np.abs(f.X), np.abs(W), c.offsets) + c.half * np.abs(ref), "Y")
+
+
+def test_not_finite_rows_stay_alone():
+    """A token with an infinity and an expert's column with a NaN: their rows and their column, nothing else."""
+    f = Four((40, 3, 70), 30, 136, "bf16", True)
+    c = f.c
+    inv = host(c.inv)
+    c.x[inv[45] // c.k, 3] = float("inf")
+    W = c.stored(c.rng.standard_normal((3, 136, 72)))
+    W[1, 9, 5] = float("nan")
+    xq, xs = store(c.x.view(1, f.rows, 136), False)
+    Wq, Ws = store(W, True)
+    Y = c.fresh(c.R, 72)
+    api.moe_ragged_gemm_mx4(xq, xs, c.S, c.inv, c.k, Wq, Ws, c.off, c.R, 3, 136, 72, Y)
+    bad = np.zeros((c.R, 72), bool)
+    bad[:113][np.isin(inv[:113] // c.k, [inv[45] // c.k])] = True
+    bad[40:43, 5] = True
+    assert np.array_equal(~np.isfinite(host(Y)), bad) and (host(Y)[113:] == 0).all()
+
+
+def test_same_bits_again_from_a_graph_and_on_another_stream():
+    f = Four((7, 0, 19), 3, 520, "bf16", True)
+    c = f.c
+    W1q, W1s, _ = f.weights(520, 2 * 1032)
+    W2q, W2s, _ = f.weights(1032, 520)
+    ws = torch.empty(api.moe_ragged_glu_mx4_workspace_bytes(c.S, c.R, 3, 520, 1032), dtype=torch.uint8, device=DEV)
+    Y = c.fresh(c.R, 520)
+    step = lambda: api.moe_ragged_glu_mx4(c.x, c.S, c.inv, c.k, W1q, W1s, W2q, W2s, c.off, c.R, 3, 520, 1032, 0, Y, ws)
+    step()
+    torch.cuda.synchronize()
+    ref = Y.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        Y.fill_(3)
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(Y, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        Y.fill_(-3)
+        ws.fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, ref)
+        step()
+        torch.cuda.synchronize()

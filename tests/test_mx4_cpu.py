@@ -1,0 +1,93 @@
+"""Microscaled 4-bit floating point: pins of the checker, and what the entry points refuse before a launch."""
+import ctypes
+
+import numpy as np
+
+from oracle import mx4_oracle as O
+from paper_2407_00599_amd import api
+
+A = ctypes.c_void_p(0x1000)        # aligned dummy pointers: never dereferenced on these paths
+U = ctypes.c_void_p(0x1004)        # misaligned
+BIG = 1 << 60
+EINVAL, EUNSUPPORTED, EALIGN, EWORKSPACE, ENULL = -1, -2, -3, -5, -6
+
+
+def test_checker_scales_and_ties():
+    # the doubled scale starts where a / scale would round to 8, between 6 and 8
+    for a, b in ((4.0, 127), (6.99, 127), (7.0, 128), (8.0, 128), (3.999, 127), (3.4, 126), (1.0, 125), (0.0, 0), (np.inf, 255), (1e-45, 0)):
+        assert O.scale_byte(a) == b, a
+    ties = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0])
+    assert list(O.code(ties, 127)) == [0, 2, 2, 4, 4, 6, 6] and list(O.code(-ties, 127)) == [8, 10, 10, 12, 12, 14, 14]
+    assert list(O.code(np.nextafter(ties, 9), 127)) == [1, 2, 3, 4, 5, 6, 7] and list(O.code(np.nextafter(ties, 0), 127)) == [0, 1, 2, 3, 4, 5, 6]
+    assert list(O.code(O.SIZES, 127)) == list(range(8)) and O.code(np.array([-0.0]), 127)[0] == 8
+
+
+def test_checker_keeps_the_nearest():
+    rng = np.random.default_rng(1)
+    x = rng.standard_normal((40, 100)) * np.exp2(rng.integers(-40, 40, (40, 1)))
+    x[3] = 0
+    q, s = O.store(x)
+    back = O.values(q, s)[:, :100]
+    step = np.repeat(np.exp2(s - 127.0), 32, 1)[:, :100]
+    m = np.abs(x) / step
+    assert m.max() < 7 and (np.abs(back - x) <= step * np.where(m > 4, 1, np.where(m > 2, 0.5, 0.25))).all() and (back[3] == 0).all()
+    assert (O.kept(back) == back).all()                                   # what is kept is kept exactly
+    lo, hi = O.kept_range(x, np.zeros_like(x))
+    assert (lo == back).all() and (hi == back).all()
+    lo, hi = O.kept_range(x, 0.1 * step)
+    assert (lo <= back).all() and (back <= hi).all()
+    assert np.isnan(O.kept(np.array([[1.0, np.nan] + [0.0] * 38]))[0, :32]).all()
+    b, f = O.pack(q, s)
+    assert b.shape == (40, 64) and f.shape == (1, 4, 40, 4)
+    assert (b[:, 0] & 15 == q[:, 0, 0]).all() and (b[:, 0] >> 4 == q[:, 0, 1]).all() and (f[0, 3, :, 0] == s[:, 3]).all() and (f[:, :, :, 1:] == 0).all()
+    assert api.mx4_shapes(2, 40, 100, False) == ((2, 40, 64), (2, 1, 4, 40, 4)) and api.mx4_shapes(1, 520, 8, True) == ((1, 8, 272), (1, 2, 4, 8, 4))
+
+
+def test_store_and_load_refusals():
+    L = api.lib()
+
+    def store(x=A, dt=1, G=1, rows=16, cols=64, tr=0, q=A, s=A):
+        return L.moe_mx4_store(x, dt, G, rows, cols, tr, q, s, None)
+
+    def load(x=A, dt=1, G=1, rows=16, cols=64, tr=0, q=A, s=A):
+        return L.moe_mx4_load(q, s, G, rows, cols, tr, x, dt, None)
+    for f in (store, load):
+        for kw in ({"dt": 2}, {"dt": -1}, {"G": 0}, {"rows": 0}, {"cols": 0}, {"tr": 2}, {"tr": -1}):
+            assert f(**kw) == EINVAL, (f, kw)
+        for kw in ({"cols": 60}, {"tr": 1, "rows": 12}, {"G": 1 << 21}, {"rows": 1 << 32}, {"tr": 1, "rows": 1 << 31}, {"G": 1 << 20, "rows": 1 << 20}):
+            assert f(**kw) == EUNSUPPORTED, (f, kw)
+        for n in ("x", "q", "s"):
+            assert f(**{n: None}) == ENULL and f(**{n: U}) == EALIGN, (f, n)
+
+
+def test_product_refusals():
+    L = api.lib()
+
+    def gemm(xq=A, xs=A, S=16, inv=A, k=2, Wq=A, Ws=A, off=A, R=32, E=4, K=64, N=128, Y=A, dt=1, ws=A, wsb=BIG):
+        return L.moe_ragged_gemm_mx4(xq, xs, S, inv, k, Wq, Ws, off, R, E, K, N, Y, dt, ws, wsb, None)
+    need = L.moe_ragged_glu_mx4_workspace_bytes(16, 32, 4, 64, 128)
+    assert need >= 32 * 128 // 2
+
+    def glu(x=A, dt=1, S=16, inv=A, k=2, W1q=A, W1s=A, W2q=A, W2s=A, off=A, R=32, E=4, M=64, H=128, act=0, Y=A, ws=A, wsb=need):
+        return L.moe_ragged_glu_mx4(x, dt, S, inv, k, W1q, W1s, W2q, W2s, off, R, E, M, H, act, Y, ws, wsb, None)
+    for f in (gemm, glu):
+        for kw in ({"dt": 2}, {"dt": -1}, {"R": 0}, {"E": 0}, {"S": 0}, {"k": 0}, {"inv": None}):
+            assert f(**kw) == EINVAL, (f, kw)
+        for kw in ({"E": 257}, {"k": 9}, {"R": (1 << 29) + 1}, {"S": 1 << 29}):
+            assert f(**kw) == EUNSUPPORTED, (f, kw)
+        assert f(inv=U) == EALIGN and f(ws=U) == EALIGN
+    for kw in ({"K": 0}, {"N": -8}):
+        assert gemm(**kw) == EINVAL, kw
+    for kw in ({"K": 60}, {"N": 12}, {"S": 1 << 28, "k": 1, "K": 512}, {"K": 1 << 20, "N": 1 << 14}, {"R": 1 << 29, "N": 512}, {"inv": None, "k": 1, "R": 1 << 28, "K": 512}):
+        assert gemm(**kw) == EUNSUPPORTED, kw
+    for n in ("xq", "xs", "Wq", "Ws", "off", "Y"):
+        assert gemm(**{n: None}) == ENULL and gemm(**{n: U}) == EALIGN, n
+    for kw in ({"M": 0}, {"H": 0}, {"act": 2}, {"act": -1}):
+        assert glu(**kw) == EINVAL, kw
+    for kw in ({"M": 60}, {"H": 12}, {"H": 1 << 29}, {"M": 1 << 18, "H": 1 << 15}, {"R": 1 << 28, "H": 512}):
+        assert glu(**kw) == EUNSUPPORTED, kw
+    for n in ("x", "W1q", "W1s", "W2q", "W2s", "off", "Y"):
+        assert glu(**{n: None}) == ENULL and glu(**{n: U}) == EALIGN, n
+    assert glu(ws=None) == EWORKSPACE and glu(wsb=need // 2) == EWORKSPACE
+    for bad in ((16, 0, 4, 64, 128), (16, 32, 0, 64, 128), (16, 32, 4, 60, 128), (-1, 32, 4, 64, 128), (1 << 40, 32, 4, 64, 128)):
+        assert L.moe_ragged_glu_mx4_workspace_bytes(*bad) == 0
