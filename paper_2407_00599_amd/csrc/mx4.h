@@ -39,6 +39,12 @@ __device__ __forceinline__ uint32_t mx4_pack(const float (&v)[8], int b) {
   q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, t[6], t[7], 1.0f, 3);
   return b == 255 ? 0u : q;
 }
+// 4 values -> 16 bits
+__device__ __forceinline__ uint32_t mx4_pack4(const float (&v)[4], int b) {
+  uint32_t q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, __builtin_amdgcn_ldexpf(v[0], 127 - b), __builtin_amdgcn_ldexpf(v[1], 127 - b), 1.0f, 0);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, __builtin_amdgcn_ldexpf(v[2], 127 - b), __builtin_amdgcn_ldexpf(v[3], 127 - b), 1.0f, 1);
+  return b == 255 ? 0u : q & 0xFFFFu;
+}
 __device__ __forceinline__ void mx4_values(uint32_t q, int b, float (&v)[8]) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
   const f32x2_t t[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.0f, 1),

@@ -44,11 +44,11 @@ __device__ __forceinline__ uint4 mx4_load16(__amdgpu_buffer_rsrc_t r, uint32_t o
 }
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
-// d += a b for 16 x 16 values and 128 k; the scales are byte OP of sa and sb
-template <int OP>
+// d += a b for 16 x 16 values and 128 k; the scales are bytes OPA of sa and OPB of sb
+template <int OPA, int OPB = OPA>
 __device__ __forceinline__ f32x4_t mx4_mfma(const uint4& a, const uint4& b, const f32x4_t& d, uint32_t sa, uint32_t sb) {
   const i32x8_t x = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, y = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, d, 4, 4, OP, (int)sa, OP, (int)sb);      // 4: e2m1
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, d, 4, 4, OPA, (int)sa, OPB, (int)sb);      // 4: e2m1
 }
 // Of a scale dword [c][q][row] the bytes of blocks that exist; the others may hold anything, also the byte of NaN, and are multiplied with zeros.
 __device__ __forceinline__ uint32_t mx4_existing(const Mx4Args& p, uint32_t four, int c, int q) {
@@ -57,5 +57,6 @@ __device__ __forceinline__ uint32_t mx4_existing(const Mx4Args& p, uint32_t four
 }
 
 void launch_mx4_few(Mx4Args a, int kind, hipStream_t st);
+void launch_mx4_tile(const Mx4Args& m, int kind, int tile, hipStream_t st);      // tiles of 256 x 256, 128 x 128 or 64 x 128
 
 }  // namespace moe

@@ -20,6 +20,20 @@ void set_summed(Mx4Args& a, int K) {
 }
 size_t tensor_bytes(int64_t n, int K) { return align_up(mx4_value_bytes(n, K), 256) + align_up(mx4_scale_bytes(n, K), 256); }
 
+// How a product is computed: 0, the kernel for few rows; 256, 128 or 64, tiles of as many rows.
+int pick_tile(int64_t R, int E, int64_t n, int K) {
+  const double rows = (double)R / E;
+  if (rows <= 32) return 0;
+  if (rows <= 80) return 64;
+  const double tiles = priced_row_tiles((int)R, E, 256) * ((n + 255) / 256);
+  return tiles < 200 ? 128 : 256;
+}
+void launch(const Mx4Args& a, int kind, hipStream_t st) {
+  const int tile = pick_tile(a.R, a.E, a.n, a.K);
+  if (tile == 0) launch_mx4_few(a, kind, st);
+  else launch_mx4_tile(a, kind, tile, st);
+}
+
 // rows of X, of one expert's W and of Y: 32-bit byte offsets
 int check_mx4_product(int64_t R, int E, int K, int64_t n) {
   MOE_REQUIRE(R >= 1 && E >= 1 && K >= 1 && n >= 1, MOE_EINVAL);
@@ -78,7 +92,7 @@ extern "C" int moe_ragged_gemm_mx4(const void* xq, const void* xs, int64_t S, co
   set_summed(a, K);
   set_source(a, inv, k, S);
   a.C = Y; a.f32 = dtype == MOE_F32;
-  launch_mx4_few(a, MX4_STORE, (hipStream_t)stream);
+  launch(a, MX4_STORE, (hipStream_t)stream);
   return check_launch();
 }
 
@@ -113,7 +127,7 @@ extern "C" int moe_ragged_glu_mx4(const void* x, int dtype, int64_t S, const int
   set_summed(a, M);
   set_source(a, inv, k, S);
   a.half = H; a.act = act; a.aq = aq; a.as = as; a.a_blocks = (int)mx4_blocks(H);
-  launch_mx4_few(a, MX4_GLU, st);
+  launch(a, MX4_GLU, st);
 
   Mx4Args y{};
   y.xq = aq; y.xs = as; y.wq = (const uint8_t*)W2q; y.ws = (const uint8_t*)W2s;
@@ -121,6 +135,6 @@ extern "C" int moe_ragged_glu_mx4(const void* x, int dtype, int64_t S, const int
   set_summed(y, H);
   set_source(y, nullptr, 1, 0);
   y.C = Y; y.f32 = dtype == MOE_F32;
-  launch_mx4_few(y, MX4_STORE, st);
+  launch(y, MX4_STORE, st);
   return check_launch();
 }
