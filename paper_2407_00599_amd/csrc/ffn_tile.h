@@ -216,21 +216,15 @@ __device__ __forceinline__ int xcd_tile(const GemmArgs& p, int x, int i, int per
   return i < full ? ((i & ~31) * 8 + x * 32) + (i & 31) : full * 8 + x * (per_xcd - full) + (i - full);
 }
 
-struct NoScales {      // of a layout whose operands have none
-  template <typename... T>
-  __device__ __forceinline__ NoScales(T&&...) {}
-};
-
 // The order of B in memory, unless a layout says otherwise: columns and k indexes as they are numbered.
 struct PlainOrder {
   template <int EPI>      // memory column of column c of a tile that starts at n0; one that does not exist: any that does
   static __device__ __forceinline__ int column(const GemmArgs& p, int n0, int c) { return n0 + c < p.Ndim ? n0 + c : n0; }
-  template <int EPI>      // the same for rows of B with k contiguous
+  template <int EPI>      // row n0 + c of B with k contiguous, or one that exists
   static __device__ __forceinline__ int row(const GemmArgs& p, int n0, int c) { return min(n0 + c, p.Ndim - 1); }
   template <int EPI>      // bytes that lie in front of k index row0 + at / 2 beside those of the k indexes before it
   static __device__ __forceinline__ uint32_t k_skip(const GemmArgs&, int, uint32_t) { return 0u; }
   static __device__ __forceinline__ int in_order(const GemmArgs&, int) { return 0; }     // added to entry `row` of a map
-  template <typename CF> using Scales = NoScales;
   static constexpr bool SCALED = false;      // 4-bit operands with a scale for every 16 bytes of a row (mx4_tile.hip)
 };
 
@@ -360,7 +354,7 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
     const int q = wave * RB + j;
     if (!B_NC) {
       b_k[j] = ((lane & 7) ^ ((4 * q + (lane >> 4)) & 7)) * 8;
-      b_req[j] = (uint32_t)L::template row<EPI>(p, n0, q * 8 + (lane >> 3)) * ldb2;
+      b_req[j] = (uint32_t)L::template row<EPI>(p, n0 + q * 8, lane >> 3) * ldb2;
       b_ko[j] = (uint32_t)b_k[j] * 2u;
     } else {
       b_k[j] = q * (64 / BCPR) + lane / BCPR;
@@ -427,28 +421,21 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
     }
     return t;
   };
-  // One request (1 KiB) of k tile kt into ring slot `slot`.  WHOLE: a k tile without missing k indexes (SCALED layouts, whose registers are the
-  // tightest: the lane's part of the address is one register, the tile's a scalar).
-  auto request_whole = [&](__amdgpu_buffer_rsrc_t r, const KTile& kt, char* to, uint32_t off) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LDS_AS void*)to, 16, (int)off, kt.row0 * 2, 0, 0);
-  };
-  auto request_a = [&](const KTile& kt, int slot, int j, auto whole_tag) {
-    if constexpr (decltype(whole_tag)::value) {
-      request_whole(rA, kt, smem + slot * CF::A_UNIT + (wave * RA + j) * 1024, a_req[j] + a_ko[j]);
-      return;
-    }
+  // One request (1 KiB) of k tile kt into ring slot `slot`.
+  auto request_a = [&](const KTile& kt, int slot, int j) {
     const uint32_t in = a_k[j] < kt.lim ? a_ko[j] : 0u;   // missing k rows are fetched from the tile's first one
     const uint32_t add = GATHER ? g_now[j] : PIECES ? ka_off[PIECES ? j : 0] : (uint32_t)kt.row0 * (A_NC ? lda2 : 2u) + in;
     dma16(rA, smem + slot * CF::A_UNIT + (wave * RA + j) * 1024, a_req[j] + add);
   };
-  auto request_b = [&](const KTile& kt, int slot, int j, auto whole_tag) {
-    if constexpr (decltype(whole_tag)::value) {
-      request_whole(rB, kt, smem + SA * CF::A_UNIT + slot * CF::B_UNIT + (wave * RB + j) * 1024, b_req[j] + b_ko[j]);
-      return;
-    }
+  auto request_b = [&](const KTile& kt, int slot, int j) {
     const uint32_t in = b_k[j] < kt.lim ? b_ko[j] : 0u;
     const uint32_t add = PIECES ? kb_off[PIECES ? j : 0] : (B_NC ? (uint32_t)kt.row0 * ldb2 : (uint32_t)kt.row0 * 2u + L::template k_skip<EPI>(p, kt.row0, in)) + in;
     dma16(rB, smem + SA * CF::A_UNIT + slot * CF::B_UNIT + (wave * RB + j) * 1024, b_req[j] + add);
+  };
+  // The same of a k tile without missing k indexes, for SCALED layouts, whose registers are the tightest: the lane's part of the address is one
+  // register, the tile's a scalar.
+  auto request_whole = [&](__amdgpu_buffer_rsrc_t r, const KTile& kt, char* to, uint32_t off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (LDS_AS void*)to, 16, (int)off, kt.row0 * 2, 0, 0);
   };
   auto ktile_at = [&](int t) -> KTile { return KTile{t * DK, p.Kdim - t * DK}; };   // row-tiled GEMMs
 
@@ -536,9 +523,11 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
   };
   // Scales: of a chunk of two k tiles, two chunks in LDS behind the tiles.  Chunk c + 1 takes the slot of chunk c - 1, whose last tile is 2 c - 1, and is
   // read from tile 2 c + 2 on: its halves come with the refill sets of tiles 2 c - 1 and 2 c.  A tile's scales are read behind the barrier in front of it,
-  // before its fragments, so that they are there when those are.
-  using SC = typename L::template Scales<CF>;
-  SC sc(p, at, g, n0, smem, lane, wave, wm, wn);
+  // each before the fragments that it goes with, so that it is there when they are.
+  auto sc = [&]() {
+    if constexpr (L::SCALED) return typename L::template Scales<CF>(p, at, g, n0, smem, lane, wave, wm, wn);
+    else return 0;
+  }();
   if constexpr (L::SCALED) {
     static_assert(KIND == KIND_NT && WK == 1 && SPT == 2 && SA == SB, "two steps to a tile, and requests that each barrier waits for");
     sc.request(0, 0);
@@ -569,12 +558,12 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
       if (st + SB >= 0) {
 #pragma unroll
         for (int j = 0; j < RB; ++j)
-          if (pro[st + SB].lim > 0) request_b(pro[st + SB], st + SB, j, std::false_type{});
+          if (pro[st + SB].lim > 0) request_b(pro[st + SB], st + SB, j);
       }
       pro_a(st + SA);
 #pragma unroll
       for (int j = 0; j < RA; ++j)
-        if (pro[st + SA].lim > 0) request_a(pro[st + SA], st + SA, j, std::false_type{});
+        if (pro[st + SA].lim > 0) request_a(pro[st + SA], st + SA, j);
     }
     if (PIECES) pro[SA - 1] = next_ktile();
     ka = pro[SA - 1];
@@ -582,8 +571,8 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
     pro_a(SA - 1);
     unrolled<0, N_LAST>([&](auto r) {
       constexpr int R = decltype(r)::value;
-      if constexpr (R < RB) { if (kb.lim > 0) request_b(kb, SB - 1, R, std::false_type{}); }
-      else { if (ka.lim > 0) request_a(ka, SA - 1, R - RB, std::false_type{}); }
+      if constexpr (R < RB) { if (kb.lim > 0) request_b(kb, SB - 1, R); }
+      else { if (ka.lim > 0) request_a(ka, SA - 1, R - RB); }
     });
     // this wave's requests for tile 0 have landed
     if (nk >= SA) __builtin_amdgcn_s_waitcnt(vmcnt_imm(IN_FLIGHT + N_LAST));
@@ -591,7 +580,10 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
     __builtin_amdgcn_s_barrier();
   }
   using K0 = std::integral_constant<int, 0>;
-  if constexpr (L::SCALED) sc.read(0);
+  if constexpr (L::SCALED) {
+    sc.read_b(0);
+    sc.template read_a<0, MB>(0);
+  }
   unrolled<0, RD::N>([&](auto op) { read_op(0, 0, K0{}, op); });
 
   auto mfma = [&](int set, int i, int j) {
@@ -605,8 +597,13 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
     unrolled<0, NREQ>([&](auto r) {
       constexpr int R = decltype(r)::value;
       if constexpr (slot_of(R) == decltype(slot_tag)::value) {
-        if constexpr (R < RB) { if (!LAST || kb.lim > 0) request_b(kb, wb, R, std::bool_constant<L::SCALED && !LAST>{}); }
-        else { if (!LAST || ka.lim > 0) request_a(ka, wa, R - RB, std::bool_constant<L::SCALED && !LAST>{}); }
+        if constexpr (L::SCALED && !LAST) {
+          if constexpr (R < RB) request_whole(rB, kb, smem + SA * CF::A_UNIT + wb * CF::B_UNIT + (wave * RB + R) * 1024, b_req[R] + b_ko[R]);
+          else request_whole(rA, ka, smem + wa * CF::A_UNIT + (wave * RA + R - RB) * 1024, a_req[R - RB] + a_ko[R - RB]);
+        } else {
+          if constexpr (R < RB) { if (!LAST || kb.lim > 0) request_b(kb, wb, R); }
+          else { if (!LAST || ka.lim > 0) request_a(ka, wa, R - RB); }
+        }
       }
     });
   };
@@ -646,7 +643,12 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
 #pragma unroll
       for (int j = 0; j < NB; ++j) ready(fb[ST & 1][j]);
       ready(fa[0]);
-      if constexpr (L::SCALED && ST == 0) sc.template take<LAST>(t);
+      if constexpr (L::SCALED) {
+        if constexpr (ST == 0) {
+          sc.template take_b<LAST>(t);
+          sc.template take_a<LAST, 0>();
+        }
+      }
       if constexpr ((KIND == KIND_TN || LAST) && !L::SCALED) {      // (4-bit values are finite, and the product of two missing blocks' scales is zero)
         if (__builtin_expect(mask != ~0ull, 0)) {   // (its code stays out of the k loop's way)
           frags_ready(ST & 1);
@@ -659,6 +661,9 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
         if constexpr (I > 0) {
           if constexpr (ST < SPT - 1 || I < BR) __builtin_amdgcn_s_waitcnt(lgkmcnt_imm(RD::newer(ST, I)));
           ready(fa[I]);
+          if constexpr (L::SCALED) {
+            if constexpr (ST == 0) sc.template take_a<LAST, I>();
+          }
         }
         unrolled<0, NB>([&](auto j) {
           constexpr int J = decltype(j)::value, AT = I * NB + J;
@@ -678,7 +683,8 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
             __builtin_amdgcn_sched_barrier(0);
             wa = sa; wb = sb;
             if constexpr (L::SCALED) {
-              sc.read(t + 1);
+              sc.read_b(t + 1);
+              sc.template read_a<0, BR>(t + 1);
               sc.request((t + 3) / 2, (t & 1) ^ 1);
             }
             if (KIND == KIND_TN) {
@@ -699,6 +705,9 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
               ka = ktile_at(t + SA);
               kb = ktile_at(t + SB);
             }
+          }
+          if constexpr (L::SCALED) {      // in front of the row's next fragment: whoever waits for that has waited for this
+            if constexpr (ST == SPT - 1 && J == NB - 1 && I >= BR) sc.template read_a<I, I + 1>(t + 1);
           }
           unrolled<0, RD::N>([&](auto op) {
             if constexpr (RD::place(ST, decltype(op)::value) == AT) {

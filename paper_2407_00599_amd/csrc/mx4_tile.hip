@@ -26,7 +26,7 @@ struct Mx4 : Ragged {
 
   template <int EPI>
   static __device__ __forceinline__ int row(const Args& p, int n0, int c) {
-    if constexpr (EPI == EPI_GLU) return min(glu_hidden(n0 + c), p.half - 1) + ((c & 16) ? p.half : 0);
+    if constexpr (EPI == EPI_GLU) return min(glu_hidden(n0 + c), p.half - 1) + (((n0 + c) & 16) ? p.half : 0);
     else return min(n0 + c, p.n - 1);
   }
   // physical rows as in Ragged::rows; of rows lane, lane + 64 of the wave tile twice the row (+ 1: a row of zeros), or OOB
@@ -59,15 +59,11 @@ struct Mx4 : Ragged {
     char* to_a;                     // this wave's place in its first plane
     char* to_b;
     int first_a, first_b, chunks, blocks, q;
-    uint32_t next_a[MB / 2], next_b[NB / 2], a[MB / 2], b[NB / 2];     // two blocks of 16 rows in a register, two bytes each
+    uint32_t a[MB], b[NB], next_b[NB], keep;      // a block's two bytes of a k tile; which bytes' blocks exist
     uint32_t lds_a, lds_b;
 
     __device__ __forceinline__ Scales(const Args& p, const Place& at, int g, int n0, char* smem, int lane, int wave, int wm, int wn)
         : chunks(p.chunks), blocks(p.blocks), q(lane >> 4) {
-#pragma unroll
-      for (int i = 0; i < MB / 2; ++i) next_a[i] = 0u;
-#pragma unroll
-      for (int j = 0; j < NB / 2; ++j) next_b[j] = 0u;
       plane_a = (uint32_t)p.x_rows * 4u;
       plane_b = (uint32_t)p.n * 4u;
       rA = make_rsrc(p.xs, plane_a * 4u * (uint32_t)chunks);
@@ -100,35 +96,41 @@ struct Mx4 : Ragged {
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rB, (LDS_AS void*)(to_b + slot + plane * PB), 4, (int)off_b, (int)((from + plane) * plane_b), 0, 0);
       }
     }
-    template <int I>      // block I of 16 rows: in the low or the high half of its register
+    template <int OFF>
     static __device__ __forceinline__ void lds_read(uint32_t& d, uint32_t addr) {
-      if constexpr (I % 2 == 0) asm volatile("ds_read_u16_d16 %0, %1 offset:%2" : "+v"(d) : "v"(addr), "n"(64 * I));
-      else asm volatile("ds_read_u16_d16_hi %0, %1 offset:%2" : "+v"(d) : "v"(addr), "n"(64 * I));
+      asm volatile("ds_read_u16 %0, %1 offset:%2" : "=v"(d) : "v"(addr), "n"(OFF));
     }
-    // the bytes of k tile t
-    __device__ __forceinline__ void read(int t) {
-      const uint32_t at = (uint32_t)((t >> 1) & 1) * SLOT + 2u * (uint32_t)(t & 1);
-      unrolled<0, MB>([&](auto i) { lds_read<decltype(i)::value>(next_a[decltype(i)::value / 2], lds_a + at); });
-      unrolled<0, NB>([&](auto j) { lds_read<decltype(j)::value>(next_b[decltype(j)::value / 2], lds_b + at); });
+    static __device__ __forceinline__ uint32_t tile_at(int t) { return (uint32_t)((t >> 1) & 1) * SLOT + 2u * (uint32_t)(t & 1); }
+    // The bytes of k tile t.  Those of rows [FROM, TO) of blocks of A go where the tile before had them, once it has multiplied the row; B's, which
+    // every row uses, wait beside them.
+    template <int FROM, int TO>
+    __device__ __forceinline__ void read_a(int t) {
+      const uint32_t at = lds_a + tile_at(t);
+      unrolled<FROM, TO>([&](auto i) { lds_read<decltype(i)::value * 64>(a[decltype(i)::value], at); });
     }
-    // They have landed.  Those of blocks that do not exist, which may be the byte of NaN, are taken as 2^-127: whatever the fragments hold there, the
-    // products with two of them are under 2^-240, zero in fp32.
+    __device__ __forceinline__ void read_b(int t) {
+      const uint32_t at = lds_b + tile_at(t);
+      unrolled<0, NB>([&](auto j) { lds_read<decltype(j)::value * 64>(next_b[decltype(j)::value], at); });
+    }
+    // B's, and row 0's of A, have landed.  Bytes of blocks that do not exist, which may be the byte of NaN, are taken as 2^-127: whatever the fragments
+    // hold there, the products with two of them are under 2^-240, zero in fp32.
     template <bool LAST>
-    __device__ __forceinline__ void take(int t) {
-      uint32_t keep = ~0u;
-      if constexpr (LAST) {
-        keep = (8 * t + q < blocks ? 0xFFu : 0u) | (8 * t + 4 + q < blocks ? 0xFF00u : 0u);
-        keep |= keep << 16;
+    __device__ __forceinline__ void take_b(int t) {
+      if constexpr (LAST) keep = (8 * t + q < blocks ? 0xFFu : 0u) | (8 * t + 4 + q < blocks ? 0xFF00u : 0u);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        asm volatile("" : "+v"(next_b[j]));
+        b[j] = LAST ? next_b[j] & keep : next_b[j];
       }
-#pragma unroll
-      for (int i = 0; i < MB / 2; ++i) { asm volatile("" : "+v"(next_a[i])); a[i] = next_a[i] & keep; }
-#pragma unroll
-      for (int j = 0; j < NB / 2; ++j) { asm volatile("" : "+v"(next_b[j])); b[j] = next_b[j] & keep; }
+    }
+    template <bool LAST, int I>
+    __device__ __forceinline__ void take_a() {
+      asm volatile("" : "+v"(a[I]));
+      if constexpr (LAST) a[I] &= keep;
     }
     template <int ST, int I, int J>
     __device__ __forceinline__ void product(f32x4_t& acc, const Frag& fb, const Frag& fa) {
-      acc = mx4_mfma<2 * (J % 2) + ST, 2 * (I % 2) + ST>(make_uint4(fb.q[0], fb.q[1], fb.q[2], fb.q[3]), make_uint4(fa.q[0], fa.q[1], fa.q[2], fa.q[3]),
-                                                         acc, b[J / 2], a[I / 2]);
+      acc = mx4_mfma<ST>(make_uint4(fb.q[0], fb.q[1], fb.q[2], fb.q[3]), make_uint4(fa.q[0], fa.q[1], fa.q[2], fa.q[3]), acc, b[J], a[I]);
     }
   };
 
@@ -207,7 +209,7 @@ struct Mx4 : Ragged {
 };
 
 template <int EPI, typename CF>
-__global__ __launch_bounds__(64 * CF::NW) void mx4_gemm(const Mx4TileArgs p) {
+__global__ __launch_bounds__(64 * CF::NW, 2) void mx4_gemm(const Mx4TileArgs p) {
   __shared__ __attribute__((aligned(1024))) char smem[CF::LDS + 2 * Mx4::Scales<CF>::SLOT];
   gemm_dma_tile<KIND_NT, EPI, CF, ROWS_PLAIN, Mx4>(p, smem, (int)blockIdx.x);
 }
