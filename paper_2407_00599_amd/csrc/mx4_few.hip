@@ -9,11 +9,11 @@
 
 namespace moe {
 
-constexpr int MX4_FEW_WAVES = 8, MX4_NC = 4;      // waves, groups of 16 columns
+constexpr int MX4_NC = 4;      // groups of 16 columns
 
-template <int KIND, int RG>
-__global__ __launch_bounds__(64 * MX4_FEW_WAVES) void mx4_few(const Mx4Args p) {
-  constexpr int NC = MX4_NC, WAVES = MX4_FEW_WAVES, TN = 16 * NC, PITCH = TN + 4, PF = RG == 1 ? 3 : 2;
+template <int KIND, int RG, int WAVES, int PF>      // groups of 16 rows that go along with one reading of the weights; units requested ahead
+__global__ __launch_bounds__(64 * WAVES) void mx4_few(const Mx4Args p) {
+  constexpr int NC = MX4_NC, TN = 16 * NC, PITCH = TN + 4;
   __shared__ float red[WAVES * 16 * PITCH];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, kg = lane >> 4;
   const int tile = (int)blockIdx.x;
@@ -145,9 +145,9 @@ __global__ __launch_bounds__(64 * MX4_FEW_WAVES) void mx4_few(const Mx4Args p) {
             uv[e] += red[(w * 16 + row) * PITCH + from + 16 + e];
           }
         uint32_t top = 0;
-        with_act(p.act, [&](auto act) {
+        with_hidden(p.act, p.f32, [&](auto act, auto wide) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = hidden < p.half ? gate_value<decltype(act)::value, false>(gv[e]) * uv[e] : 0.f;
+          for (int e = 0; e < 8; ++e) a[e] = hidden < p.half ? mx4_hidden<decltype(act)::value, decltype(wide)::value>(gv[e], uv[e]) : 0.f;
         });
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(a[e]) & 0x7FFFFFFFu);
@@ -168,10 +168,18 @@ void launch_mx4_few(Mx4Args a, int kind, hipStream_t st) {
   a.tiles_n = kind == MX4_GLU ? (a.half + 8 * MX4_NC - 1) / (8 * MX4_NC) : (a.n + 16 * MX4_NC - 1) / (16 * MX4_NC);
   const dim3 grid((unsigned)(a.E * a.tiles_n + (kind == MX4_STORE ? ZERO_SHARES : 0)));
   const bool one = a.R <= 8 * (int64_t)a.E || a.R <= 16;
-  auto launch = [&](auto k, auto rg) { hipLaunchKernelGGL((mx4_few<decltype(k)::value, decltype(rg)::value>), grid, dim3(64 * MX4_FEW_WAVES), 0, st, a); };
+  auto launch = [&](auto k, auto rg, auto waves, auto pf) {
+    constexpr int W = decltype(waves)::value;
+    hipLaunchKernelGGL((mx4_few<decltype(k)::value, decltype(rg)::value, W, decltype(pf)::value>), grid, dim3(64 * W), 0, st, a);
+  };
   using std::integral_constant;
-  if (kind == MX4_GLU) one ? launch(integral_constant<int, MX4_GLU>{}, integral_constant<int, 1>{}) : launch(integral_constant<int, MX4_GLU>{}, integral_constant<int, 2>{});
-  else one ? launch(integral_constant<int, MX4_STORE>{}, integral_constant<int, 1>{}) : launch(integral_constant<int, MX4_STORE>{}, integral_constant<int, 2>{});
+  using W4 = integral_constant<int, 4>;
+  auto with_kind = [&](auto rg, auto pf) {
+    if (kind == MX4_GLU) launch(integral_constant<int, MX4_GLU>{}, rg, W4{}, pf);
+    else launch(integral_constant<int, MX4_STORE>{}, rg, W4{}, pf);
+  };
+  if (one) with_kind(integral_constant<int, 1>{}, integral_constant<int, 1>{});
+  else with_kind(integral_constant<int, 2>{}, integral_constant<int, 1>{});
 }
 
 }  // namespace moe

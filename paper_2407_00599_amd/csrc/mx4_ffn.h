@@ -23,7 +23,7 @@ struct Mx4Args {
   int R, E, n, K, blocks, chunks;  // blocks of 32 and chunks of 512 in K
   int64_t x_rows;                  // rows of X
   void* C;                         // Y, leading dimension n
-  int f32;                         // Y is fp32, otherwise bf16
+  int f32;                         // Y (of a first product: the activations) in fp32, otherwise bf16
   int half, act;                   // gated first product: hidden columns
   uint8_t* aq;                     // its 4-bit results, of R rows
   uint8_t* as;
@@ -35,6 +35,32 @@ __device__ __forceinline__ int offset(const Mx4Args& p, int e) { return min(max(
 __device__ __forceinline__ int token(const Mx4Args& p, int iv) {
   const uint32_t tok = p.gather_k == 1 ? (uint32_t)iv : __umulhi((uint32_t)iv, p.gather_magic);
   return iv >= 0 && (int64_t)tok < p.gather_rows ? (int)tok : -1;
+}
+
+// act(g) u on its way to 4 bits.  With fp32 activations in 64 bits, because a value next to the border between two codes decides which one is kept, and
+// handed on rounded to odd: towards zero, with the last bit set where that was not exact, which any rounding to fewer bits decides as for the value
+// itself.  With bf16 ones in fp32, SiLU by the exponential and the reciprocal of the hardware.
+__device__ __forceinline__ float round_to_odd(double d) {
+  const float f = (float)d;
+  const uint32_t bits = __float_as_uint(f);
+  return (double)f == d || d != d ? f : __uint_as_float((fabs((double)f) > fabs(d) ? bits - 1u : bits) | 1u);
+}
+template <int ACT, bool WIDE>
+__device__ __forceinline__ float mx4_hidden(float g, float u) {
+  if constexpr (WIDE) {
+    const double z = (double)g;
+    const double a = ACT == MOE_ACT_SILU ? z / (1.0 + exp(-z)) : 0.5 * z * erfc(z * -0.70710678118654752440);
+    return round_to_odd(a * (double)u);
+  }
+  return gate_value<ACT, ACT == MOE_ACT_SILU>(g) * u;
+}
+// f(integral_constant<int, ACT>, bool_constant<WIDE>)
+template <typename F>
+__device__ __forceinline__ void with_hidden(int act, int wide, F&& f) {
+  with_act(act, [&](auto a) {
+    if (wide) f(a, std::true_type{});
+    else f(a, std::false_type{});
+  });
 }
 
 // 16 bytes at off + at, `at` the same in all lanes; OOB: zeros (the range is checked without `at`, against a range that is shorter by it)
@@ -57,6 +83,6 @@ __device__ __forceinline__ uint32_t mx4_existing(const Mx4Args& p, uint32_t four
 }
 
 void launch_mx4_few(Mx4Args a, int kind, hipStream_t st);
-void launch_mx4_tile(const Mx4Args& m, int kind, int tile, hipStream_t st);      // tiles of 256 x 256, 128 x 128 or 64 x 128
+void launch_mx4_tile(const Mx4Args& m, int kind, int tile, hipStream_t st);      // tiles of 256 x 256 or 128 x 128
 
 }  // namespace moe

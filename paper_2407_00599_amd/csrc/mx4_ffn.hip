@@ -1,6 +1,8 @@
 // Expert products and the gated expert FFN over ragged rows from microscaled 4-bit values (mx4.h):
 //   Y = X W of each row's expert, both in 4 bits, fp32 sums of exact products;
 //   the FFN: token rows to 4 bits, G and U from the two halves of W1, A = act(G) U to 4 bits, Y = A W2.
+#include <math.h>
+
 #include "mx4_ffn.h"
 
 namespace moe {
@@ -20,13 +22,32 @@ void set_summed(Mx4Args& a, int K) {
 }
 size_t tensor_bytes(int64_t n, int K) { return align_up(mx4_value_bytes(n, K), 256) + align_up(mx4_scale_bytes(n, K), 256); }
 
-// How a product is computed: 0, the kernel for few rows; 256, 128 or 64, tiles of as many rows.
+// How a product is computed: 0, the kernel for few rows; 128 or 256, square tiles.  Experts of few rows are bound by their weights' bytes, which the kernel
+// for few rows reads fastest, but again for every 32 rows: 8 experts x 4096 x 14336 with 4, 16, 32 and 64 rows each 47, 59, 86 and 131 us, on
+// tiles of 128 58, 59, 61 and 64; 64 x 2048 x 2048 with 4, 16 and 32 28, 38 and 58, on tiles 33, 35 and 37.  Of the tiles the small ones waste less of
+// experts with few rows and fill the chip with fewer of them: rounds of tiles on the chip, each of k tiles of 256 and what is outside the k loop (us,
+// measured; with few and with all compute units busy).  8 x 4096 x 14336 with 64, 256, 1024 and 4096 rows each, tiles of 128 64, 124, 376 and
+// 1353 us, of 256 76, 111, 290 and 1092; 1 x 2048 x 8192 with 1024 and 4096 rows 18 and 55, 22 and 44.  Tiles of 64 x 128 were nowhere the fastest.
+struct Mx4TileCost {
+  int tile, per_cu;
+  float k_few, k_all, fixed;
+};
+constexpr Mx4TileCost MX4_TILES[] = {{256, 1, 1.25f, 1.75f, 8.f}, {128, 2, 0.75f, 1.10f, 6.f}};
+constexpr int MX4_FEW_ROWS = 16;      // of an expert, on average
 int pick_tile(int64_t R, int E, int64_t n, int K) {
-  const double rows = (double)R / E;
-  if (rows <= 32) return 0;
-  if (rows <= 80) return 64;
-  const double tiles = priced_row_tiles((int)R, E, 256) * ((n + 255) / 256);
-  return tiles < 200 ? 128 : 256;
+  if (R <= (int64_t)MX4_FEW_ROWS * E) return 0;
+  const float nk = (float)((K + 255) / 256), cu = (float)num_cus();
+  int best = 0;
+  float best_t = 0.f;
+  for (const Mx4TileCost& c : MX4_TILES) {
+    const double rows = E == 1 ? (double)((R + c.tile - 1) / c.tile) : priced_row_tiles((int)R, E, c.tile);
+    const float tiles = (float)rows * (float)((n + c.tile - 1) / c.tile);
+    const float busy = c.per_cu == 1 ? tiles / cu : (tiles - cu) / cu;
+    const float k = c.k_few + (c.k_all - c.k_few) * fminf(fmaxf(busy, 0.f), 1.f);
+    const float t = ceilf(tiles / (cu * c.per_cu)) * (nk * k + c.fixed);
+    if (best == 0 || t < best_t) { best_t = t; best = c.tile; }
+  }
+  return best;
 }
 void launch(const Mx4Args& a, int kind, hipStream_t st) {
   const int tile = pick_tile(a.R, a.E, a.n, a.K);
@@ -126,7 +147,7 @@ extern "C" int moe_ragged_glu_mx4(const void* x, int dtype, int64_t S, const int
   a.off = offsets; a.R = (int)R; a.E = E; a.n = 2 * H;
   set_summed(a, M);
   set_source(a, inv, k, S);
-  a.half = H; a.act = act; a.aq = aq; a.as = as; a.a_blocks = (int)mx4_blocks(H);
+  a.half = H; a.act = act; a.f32 = dtype == MOE_F32; a.aq = aq; a.as = as; a.a_blocks = (int)mx4_blocks(H);
   launch(a, MX4_GLU, st);
 
   Mx4Args y{};

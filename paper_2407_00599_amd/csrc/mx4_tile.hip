@@ -145,7 +145,7 @@ struct Mx4 : Ragged {
       // pieces of 32 columns are 16 of the gate and 16 of the up projection: two of them are 32 hidden columns, one block of A
       static_assert(NBK == 2, "a wave's hidden columns are one block");
       const int h0 = nbase / 2, block = h0 / MX4_BLOCK;
-      with_act(p.act, [&](auto act) {
+      with_hidden(p.act, p.f32, [&](auto act, auto wide) {
 #pragma unroll
         for (int i = 0; i < AM; ++i) {
           const uint32_t o = row_of(mshift + 16 * i, l16);
@@ -157,7 +157,7 @@ struct Mx4 : Ragged {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float g = acc[i][2 * j][e], u = acc[i][2 * j + 1][e];
-              v[j][e] = zero || h0 + 16 * j + 4 * kg >= p.half ? 0.f : gate_value<decltype(act)::value, false>(g) * u;
+              v[j][e] = zero || h0 + 16 * j + 4 * kg >= p.half ? 0.f : mx4_hidden<decltype(act)::value, decltype(wide)::value>(g, u);
               top = max(top, __float_as_uint(v[j][e]) & 0x7FFFFFFFu);
             }
           top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
@@ -216,7 +216,6 @@ __global__ __launch_bounds__(64 * CF::NW, 2) void mx4_gemm(const Mx4TileArgs p) 
 
 using Mx4Tile256 = TileCfg<256, 256, 2, 4, 1, 2, 2>;
 using Mx4Tile128 = TileCfg<128, 128, 2, 2, 1, 2, 2>;
-using Mx4Tile64 = TileCfg<64, 128, 1, 2, 1, 2, 2>;
 
 void launch_mx4_tile(const Mx4Args& m, int kind, int tile, hipStream_t st) {
   Mx4TileArgs a{};
@@ -241,8 +240,7 @@ void launch_mx4_tile(const Mx4Args& m, int kind, int tile, hipStream_t st) {
     else hipLaunchKernelGGL((mx4_gemm<EPI_STORE, CF>), grid, dim3(64 * CF::NW), 0, st, a);
   };
   if (tile == 256) launch(Mx4Tile256{});
-  else if (tile == 128) launch(Mx4Tile128{});
-  else launch(Mx4Tile64{});
+  else launch(Mx4Tile128{});
 }
 
 }  // namespace moe
