@@ -246,24 +246,33 @@ class DroplessBlock:
     norm -> gate -> plan of the ragged rows -> expert FFN over them -> combine -> norm, gate, residual scale and residual, and the
     mirror image backward.  The rows of all experts are one buffer of k blocks of S rows to the combine calls.
 
-    `forward` keeps what `backward` reads in the block's buffers until the next `forward`: of the hidden layer one byte of pre-activation a
-    value and a scale byte per 32, for each of the S k rows; beside it the experts' rows, the routing, u, h and the statistics.  x and
-    the parameters are kept by reference.  `infer` keeps nothing and has buffers of its own for what it writes (the activation [S k, H] and the
+    ffn: "gelu", experts of one projection and erf GeLU, or "swiglu" or "geglu", gated experts: A = act(X W1[gate]) X W1[up].
+
+    `forward` keeps what `backward` reads in the block's buffers until the next `forward`: of the hidden layer of "gelu" one byte of pre-activation a
+    value and a scale byte per 32, of gated experts both projections in `dtype`, for each of the S k rows; beside it the experts' rows, the
+    routing, u, h and the statistics.  x and the parameters are kept by reference.  `infer` keeps nothing and has buffers of its own for what it writes (the activation [S k, H] and the
     workspace are scratch of every call), so it may run between `forward` and `backward`.  Each returns a buffer that its next
     call overwrites.  training=False: a block that only serves, without the gradients' and the kept buffers.
 
-    params: w1, b1, w2, b2 (norm weights, fp32 [M]; the biases only for "layer"), Wg [M, E] fp32, W1 [E, M, H], W2 [E, H, M], and
-    gate: fp32 [M] ("channel"), [S] ("token") or None."""
+    params: w1, b1, w2, b2 (norm weights, fp32 [M]; the biases only for "layer"), Wg [M, E] fp32, W1 [E, M, H] (gated: [E, M, 2 H], the gate's
+    columns and behind them the up projection's), W2 [E, H, M], and gate: fp32 [M] ("channel"), [S] ("token") or None.
+    `quantise(params)` gives the parameters of gated experts with W1 and W2 in microscaled 4-bit floating point, for `infer`."""
 
     NORMS = {"rms": api.MOE_NORM_RMS, "layer": api.MOE_NORM_LAYER}
     GATES = {"none": api.MOE_GATE_NONE, "channel": api.MOE_GATE_CHANNEL, "token": api.MOE_GATE_TOKEN}
+    FFNS = {"gelu": None, "swiglu": api.MOE_ACT_SILU, "geglu": api.MOE_ACT_GELU}     # the activation of gated experts
+    MX4 = ("W1q", "W1s", "W2q", "W2s")
 
     def __init__(self, S, M, H, E, k, dtype=torch.bfloat16, norm="rms", gate="none", alpha=1.0, eps=1e-5, norm_topk=-1,
-                 device="cuda:0", training=True):
+                 device="cuda:0", training=True, ffn="gelu"):
         self.S, self.M, self.H, self.E, self.k = S, M, H, E, k
         self.alpha, self.eps, self.norm_topk = alpha, eps, norm_topk
         if norm not in self.NORMS or gate not in self.GATES:
             raise ValueError(f"norm is one of {list(self.NORMS)}, gate one of {list(self.GATES)}: got {norm!r}, {gate!r}")
+        if ffn not in self.FFNS:
+            raise ValueError(f"ffn is one of {list(self.FFNS)}: got {ffn!r}")
+        self.act = self.FFNS[ffn]
+        gated = self.act is not None
         self.layer = norm == "layer"
         self.kind, self.gate_kind = self.NORMS[norm], self.GATES[gate]
         self.R = R = S * k
@@ -281,17 +290,22 @@ class DroplessBlock:
         if training:
             self.__dict__.update(written_by_a_pass())
             self.mean1, self.rstd1, self.mean2, self.rstd2 = (e(S, dt=f32) for _ in range(4))
-            self.Zq = e(R, H, dt=torch.int8); self.Zs = e(R, (H + 31) // 32, dt=torch.uint8)
+            if gated:
+                self.Z = e(R, 2 * H)
+            else:
+                self.Zq = e(R, H, dt=torch.int8); self.Zs = e(R, (H + 31) // 32, dt=torch.uint8)
             self.dh, self.du, self.dx = e(S, M), e(S, M), e(S, M)
             self.dY, self.dX, self.dw = e(R, M), e(R, M), e(S, k, dt=f32)
-            self.dW1, self.dW2 = e(E, M, H), e(E, H, M)
+            self.dW1, self.dW2 = e(E, M, 2 * H if gated else H), e(E, H, M)
             self.dlogits = e(S, E, dt=f32); self.dWg = e(M, E, dt=f32)
             self.dw1, self.db1, self.dw2, self.db2 = (e(M, dt=f32) for _ in range(4))
             self.dgate = None if gate == "none" else e(M if gate == "channel" else S, dt=f32)
-        nbytes = [api.moe_gate_workspace_bytes(S, E, k), api.moe_ragged_ffn_workspace_bytes(self.code, R, E, M, H, 1, 0), 256]
+        ffn_bytes = api.moe_ragged_glu_workspace_bytes if gated else api.moe_ragged_ffn_workspace_bytes
+        nbytes = [api.moe_gate_workspace_bytes(S, E, k), ffn_bytes(self.code, R, E, M, H, 1, 0), 256]
+        if gated:
+            nbytes += [api.moe_ragged_glu_mx4_workspace_bytes(S, R, E, M, H)]
         if training:
-            nbytes += [api.moe_gate_bwd_workspace_bytes(S, M, E), api.moe_norm_bwd_workspace_bytes(S, M),
-                       api.moe_ragged_ffn_workspace_bytes(self.code, R, E, M, H, 1, 1)]
+            nbytes += [api.moe_gate_bwd_workspace_bytes(S, M, E), api.moe_norm_bwd_workspace_bytes(S, M), ffn_bytes(self.code, R, E, M, H, 1, 1)]
         self.ws = torch.empty(max(nbytes), dtype=torch.uint8, device=device)
 
     def _moe(self, x, p, t, keep):
@@ -305,18 +319,42 @@ class DroplessBlock:
         # a token asks for an expert once: capacity S drops nothing
         api.moe_gate_topk(t.u, p["Wg"], None, S, M, E, k, S, 0, 1, self.norm_topk, t.logits, t.idx, t.slot, t.w, self.inv, t.counts, self.ws)
         api.moe_ragged_plan(t.idx, t.slot, t.counts, S, E, k, S, t.offsets, t.row_idx, t.row_slot, t.row_inv)
-        api.moe_ragged_ffn_fwd(t.u, S, t.row_inv, k, p["W1"], p["W2"], t.offsets, R, E, M, self.H, 0, 1,
-                               self.Zq if keep else None, self.Zs if keep else None, self.A, t.Y, self.ws)
+        if self.act is None:
+            api.moe_ragged_ffn_fwd(t.u, S, t.row_inv, k, p["W1"], p["W2"], t.offsets, R, E, M, self.H, 0, 1,
+                                   self.Zq if keep else None, self.Zs if keep else None, self.A, t.Y, self.ws)
+        elif "W1q" in p:
+            api.moe_ragged_glu_mx4(t.u, S, t.row_inv, k, *(p[n] for n in self.MX4), t.offsets, R, E, M, self.H, self.act, t.Y, self.ws)
+        else:
+            api.moe_ragged_glu_fwd(t.u, S, t.row_inv, k, p["W1"], p["W2"], t.offsets, R, E, M, self.H, 0, 1, self.act,
+                                   self.Z if keep else None, self.A, t.Y, self.ws)
         api.moe_combine_fwd(t.Y, 1, S, M, k, k, S, t.row_idx, t.row_slot, t.w, t.h)
         api.moe_norm_residual_fwd(t.h, x, S, M, self.kind, p["w2"], b2, p.get("gate"), self.gate_kind, self.alpha, self.eps, t.y, m2, r2)
         return t.y
 
     def infer(self, x, params):
+        if self.act is None and "W1q" in params:
+            raise ValueError("experts of one projection are not served from 4 bits")
         return self._moe(x, params, self.serving, keep=False)
+
+    def quantise(self, params):
+        """params for `infer` with the experts' W1 and W2 in 4 bits, 17/32 bytes a weight; the others are the same tensors."""
+        if self.act is None:
+            raise ValueError('quantise: ffn="swiglu" or "geglu"')
+        p = {n: v for n, v in params.items() if n not in ("W1", "W2")}
+        for name, rows, cols in (("W1", self.M, 2 * self.H), ("W2", self.H, self.M)):
+            W = params[name]
+            if tuple(W.shape) != (self.E, rows, cols):
+                raise ValueError(f"{name} has the shape {tuple(W.shape)}, not {(self.E, rows, cols)}")
+            q, s = (torch.empty(shape, dtype=torch.uint8, device=W.device) for shape in api.mx4_shapes(self.E, rows, cols, True))
+            api.moe_mx4_store(W, self.E, rows, cols, True, q, s)
+            p[name + "q"], p[name + "s"] = q, s
+        return p
 
     def forward(self, x, params):
         if not self.training:
             raise RuntimeError("a block with training=False has no forward pass that is kept: use infer")
+        if "W1q" in params:
+            raise ValueError("parameters in 4 bits have no gradients: use infer")
         self.x = None                 # a call that is refused half way leaves nothing to go back through
         y = self._moe(x, params, self, keep=True)
         self.x, self.p = x, params
@@ -331,8 +369,12 @@ class DroplessBlock:
         api.moe_norm_residual_bwd(dy, self.h, S, M, self.kind, p["w2"], only(p.get("b2")), p.get("gate"), self.gate_kind, self.alpha,
                                   only(self.mean2), self.rstd2, self.dh, self.dw2, only(self.db2), self.dgate, self.ws)
         api.moe_combine_bwd(self.dh, self.Y, 1, S, M, k, k, S, self.row_idx, self.row_slot, self.row_inv, self.w, self.dY, self.dw)
-        api.moe_ragged_ffn_bwd(self.dY, self.u, S, self.row_inv, k, self.Zq, self.Zs, p["W1"], p["W2"], self.offsets, R, E, M, self.H,
-                               0, 1, self.dX, self.dW1, self.dW2, self.ws)
+        if self.act is None:
+            api.moe_ragged_ffn_bwd(self.dY, self.u, S, self.row_inv, k, self.Zq, self.Zs, p["W1"], p["W2"], self.offsets, R, E, M, self.H,
+                                   0, 1, self.dX, self.dW1, self.dW2, self.ws)
+        else:
+            api.moe_ragged_glu_bwd(self.dY, self.u, S, self.row_inv, k, self.Z, p["W1"], p["W2"], self.offsets, R, E, M, self.H, 0, 1,
+                                   self.act, self.dX, self.dW1, self.dW2, self.ws)
         api.moe_combine_fwd(self.dX, 1, S, M, k, k, S, self.row_idx, self.row_slot, None, self.du)
         api.moe_gate_bwd(self.dw, self.w, self.idx, self.logits, self.u, p["Wg"], S, M, E, k, self.norm_topk, self.dlogits, self.dWg,
                          None, self.du, 1, self.ws)
