@@ -268,6 +268,14 @@ void launch_glu_backward(RaggedArgs dx, RaggedArgs w2, RaggedArgs wg, RaggedArgs
   }
 }
 
+// The kernels for few rows: as for the FFN with one projection, their number has a bound because an expert's weights are read again for every 16 of them.
+// Tiles and this, forward call: 2 rows, 8 experts x 1024 x 4096 26.4 and 19.9 us, 8 x 4096 x 14336 166 and 131; 64 rows 57.5 and 50.1, 567 and 509; but with
+// few weights the tiles' two launches are shorter, 2 rows of 64 x 2048 x 2048 24.0 and 24.6, 16 rows of 1 x 1024 x 2816 21.0 and 23.2, 32 rows of
+// 8 x 512 x 1536 18.9 and 19.3.
+bool few_rows_glu(int dtype, int64_t R, int E, int M, int Hl) {
+  return dtype == MOE_BF16 && (R <= 32 || (R <= 64 && R <= 8 * (int64_t)E)) && Hl >= 2 * (int64_t)M && std::min<int64_t>(R, E) * M * Hl >= 1 << 23;
+}
+
 int check_glu(int dtype, int64_t R, int E, int M, int H, int esp_idx, int n_esp) {
   MOE_REQUIRE(M >= 1 && H >= 1 && n_esp >= 1 && esp_idx >= 0 && esp_idx < n_esp && H % n_esp == 0, MOE_EINVAL);
   MOE_REQUIRE(H <= 1 << 28, MOE_EUNSUPPORTED);      // 2 H and its tiles are counted in 32 bits
@@ -288,7 +296,7 @@ extern "C" size_t moe_ragged_glu_workspace_bytes(int dtype, int64_t R, int E, in
   if (check_glu(dtype, R, E, M, H, 0, n_esp) != MOE_OK) return 0;
   const int Hl = H / n_esp;
   if (backward) return dz_bytes(dtype, R, Hl) + hidden_bytes(dtype, R, Hl) + glu_part_bytes(glu_parts(dtype, R, E, M, Hl), E, M, Hl);
-  return row_part_bytes(row_parts(dtype, R, E, Hl, M), R, M);
+  return few_rows_glu(dtype, R, E, M, Hl) ? few_rows_bytes(R, E, M, Hl) : row_part_bytes(row_parts(dtype, R, E, Hl, M), R, M);
 }
 
 extern "C" int moe_ragged_glu_fwd(const void* x, int dtype, int64_t S, const int32_t* inv, int k, const void* W1, const void* W2,
@@ -314,6 +322,12 @@ extern "C" int moe_ragged_glu_fwd(const void* x, int dtype, int64_t S, const int
   y.B = W2; y.ldb = M; y.b_goff = (int64_t)H * M; y.b_off = h0 * M;
   y.C = Y; y.ldc = M;
   y.Mdim = y.R; y.Ndim = M; y.Kdim = Hl;
+  if (Z == nullptr && few_rows_glu(dtype, R, E, M, Hl) && ws != nullptr && ws_bytes >= few_rows_bytes(R, E, M, Hl)) {
+    buffer_sizes(a, false);
+    buffer_sizes(y, false);
+    launch_few_rows(a, y, true, ws, st);
+    return check_launch();
+  }
   if (Z) launch_glu<KIND_NN, EPI_GLU_KEEP>(a, dtype, st);
   else launch_glu<KIND_NN, EPI_GLU>(a, dtype, st);
   launch_second(y, dtype, ws, ws_bytes, st);

@@ -12,7 +12,7 @@ namespace moe {
 constexpr int MX4_NC = 4;      // groups of 16 columns
 
 template <int KIND, int RG, int WAVES, int PF>      // groups of 16 rows that go along with one reading of the weights; units requested ahead
-__global__ __launch_bounds__(64 * WAVES) void mx4_few(const Mx4Args p) {
+__global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
   constexpr int NC = MX4_NC, TN = 16 * NC, PITCH = TN + 4;
   __shared__ float red[WAVES * 16 * PITCH];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, kg = lane >> 4;
@@ -43,15 +43,13 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few(const Mx4Args p) {
     ws_off[j] = ok ? (uint32_t)kg * w_scales + row * 4u : OOB;
   }
   for (int m0 = 0; m0 < n; m0 += 16 * RG) {
-    uint32_t x_off[RG], xs_off[RG];
+    int entry[RG];             // of the row map; asked for first, waited for behind the weights' requests
 #pragma unroll
     for (int q = 0; q < RG; ++q) {
-      const int r = m0 + 16 * q + c16;
-      int row = r < n ? lo + r : -1;
-      if (p.gather != nullptr && row >= 0) row = token(p, p.gather[row]);
-      x_off[q] = row >= 0 ? (uint32_t)row * pitch + (uint32_t)kg * 16u : OOB;
-      xs_off[q] = row >= 0 ? (uint32_t)kg * x_scales + (uint32_t)row * 4u : OOB;
+      entry[q] = lo + min(m0 + 16 * q + c16, n - 1);
+      if (p.gather != nullptr) entry[q] = p.gather[entry[q]];
     }
+    uint32_t x_off[RG], xs_off[RG];
     struct Unit {
       uint4 w[NC][2], x[RG][2];
       uint32_t ws[NC], xs[RG];
@@ -59,21 +57,23 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few(const Mx4Args p) {
     Unit u[PF];
     // Offsets of this lane's rows are fixed, the unit's part of an address is in a scalar register.
     // No request and no product stands in a branch: their registers would be copied, and waited for, where the branches meet.
-    auto request = [&](Unit& d, int s) {           // blocks behind the last one: zeros
+    auto request_w = [&](Unit& d, int s) {         // blocks behind the last one: zeros
+      const int at = min(s, units - 1);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool in = 8 * s + 4 * h + kg < p.blocks;        // so is every block of a unit behind the last one
-        const int at = min(s, units - 1) * 128 + h * 64;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < NC; ++j) d.w[j][h] = mx4_load16(rW, in ? w_off[j] : OOB, at);
+        for (int j = 0; j < NC; ++j) d.w[j][h] = mx4_load16(rW, 8 * s + 4 * h + kg < p.blocks ? w_off[j] : OOB, at * 128 + h * 64);
 #pragma unroll
-        for (int q = 0; q < RG; ++q) d.x[q][h] = mx4_load16(rX, in ? x_off[q] : OOB, at);
-      }
-      const uint32_t c = (uint32_t)min(s, units - 1) >> 1;
+      for (int j = 0; j < NC; ++j) d.ws[j] = __builtin_amdgcn_raw_buffer_load_b32(rWS, (int)ws_off[j], (int)((uint32_t)at / 2u * 4u * w_scales), 0);
+    };
+    auto request_x = [&](Unit& d, int s) {
+      const int at = min(s, units - 1);
 #pragma unroll
-      for (int j = 0; j < NC; ++j) d.ws[j] = __builtin_amdgcn_raw_buffer_load_b32(rWS, (int)ws_off[j], (int)(c * 4u * w_scales), 0);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int q = 0; q < RG; ++q) d.xs[q] = __builtin_amdgcn_raw_buffer_load_b32(rXS, (int)xs_off[q], (int)(c * 4u * x_scales), 0);
+        for (int q = 0; q < RG; ++q) d.x[q][h] = mx4_load16(rX, 8 * s + 4 * h + kg < p.blocks ? x_off[q] : OOB, at * 128 + h * 64);
+#pragma unroll
+      for (int q = 0; q < RG; ++q) d.xs[q] = __builtin_amdgcn_raw_buffer_load_b32(rXS, (int)xs_off[q], (int)((uint32_t)at / 2u * 4u * x_scales), 0);
     };
     f32x4_t acc[RG][NC];
 #pragma unroll
@@ -82,7 +82,19 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few(const Mx4Args p) {
       for (int j = 0; j < NC; ++j) acc[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < PF; ++i) {
-      request(u[i], wave + WAVES * i);
+      request_w(u[i], wave + WAVES * i);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int q = 0; q < RG; ++q) {
+      int row = m0 + 16 * q + c16 < n ? entry[q] : -1;
+      if (p.gather != nullptr && row >= 0) row = token(p, row);
+      x_off[q] = row >= 0 ? (uint32_t)row * pitch + (uint32_t)kg * 16u : OOB;
+      xs_off[q] = row >= 0 ? (uint32_t)kg * x_scales + (uint32_t)row * 4u : OOB;
+    }
+#pragma unroll
+    for (int i = 0; i < PF; ++i) {
+      request_x(u[i], wave + WAVES * i);
       __builtin_amdgcn_sched_barrier(0);
     }
     for (int s0 = wave; s0 < units; s0 += WAVES * PF) {
@@ -104,7 +116,8 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few(const Mx4Args p) {
           }
         }
         __builtin_amdgcn_sched_barrier(0);         // or the next unit's registers are taken before these are free
-        request(d, s + WAVES * PF);
+        request_w(d, s + WAVES * PF);
+        request_x(d, s + WAVES * PF);
         __builtin_amdgcn_sched_barrier(0);
       }
     }

@@ -155,9 +155,9 @@ __device__ __forceinline__ int glu_column(const RaggedArgs& p, int n0, int c) {
   return h < p.half ? h + ((c & 16) ? p.up : 0) : 0;
 }
 
-// The FFN of few rows (ragged_few.hip): bf16, nothing kept for a backward pass; ws of few_rows_bytes().
+// The FFN of few rows (ragged_few.hip), with one projection or gated: bf16, nothing kept for a backward pass; ws of few_rows_bytes().
 size_t few_rows_bytes(int64_t R, int E, int M, int Hl);
-void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, void* ws, hipStream_t st);
+void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, bool gated, void* ws, hipStream_t st);
 
 // fp32 products on the fp32 matrix cores (ragged_f32.hip); EPI_PART: the reduction in a.splits parts, which go to a.part
 constexpr int F32_TILE = 64, KC = 32;      // tile, k chunk

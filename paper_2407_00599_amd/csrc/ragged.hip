@@ -341,7 +341,7 @@ extern "C" int moe_ragged_ffn_fwd(const void* x, int dtype, int64_t S, const int
   if (Zq == nullptr && few_rows(dtype, R, E, M, Hl) && ws != nullptr && ws_bytes >= few_rows_bytes(R, E, M, Hl)) {
     buffer_sizes(a, false);
     buffer_sizes(y, false);
-    launch_few_rows(a, y, ws, st);
+    launch_few_rows(a, y, false, ws, st);
     return check_launch();
   }
   if (Zq) launch_rows<KIND_NN, EPI_GELU8>(a, dtype, st);

@@ -25,12 +25,12 @@ constexpr int FEW_PART_STEPS = 8;     // steps of a part at least
 template <int NCL> struct Cols;
 template <> struct Cols<4> {
   u32x2_t v;
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off) { v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, 0, 0); }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t at = 0) { v = __builtin_amdgcn_raw_buffer_load_b64(r, (int)off, (int)at, 0); }
   __device__ __forceinline__ uint32_t pair(int i) const { return v[i]; }
 };
 template <> struct Cols<8> {
   u32x4_t v;
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off) { v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0); }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t at = 0) { v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, (int)at, 0); }
   __device__ __forceinline__ uint32_t pair(int i) const { return v[i]; }
 };
 
@@ -145,6 +145,130 @@ __device__ __forceinline__ void store_pair(const FewArgs& p, int row, int col, c
   *reinterpret_cast<uint32_t*>(reinterpret_cast<bf16_t*>(p.C) + (int64_t)row * p.ldc + col) = pack_bf16x2(v.x, v.y);
 }
 
+// The gated first product: a lane reads NCL columns of the gate and the NCL of the up projection that belong to them, RG groups of 16 rows go along.
+// No request stands in a branch (their registers would be copied, and waited for, where the branches meet): steps behind the last one are zeros, and a
+// lane's offsets are fixed, the step's part of an address being a scalar.  The sums of the two halves meet in LDS one after the other.
+template <int NCL, int RG, int WAVES, int PF>      // PF steps requested ahead
+__device__ __forceinline__ void few_rows_glu(const FewArgs& p, float* red, int g, int lo, int n, int m0, int h0) {
+  constexpr int TH = 16 * NCL, PITCH = TH + 4, UNITS = 16 * TH / 2 / (64 * WAVES);
+  static_assert(UNITS * 64 * WAVES == 16 * TH / 2, "pairs of hidden columns of 16 rows");
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15, kg = lane >> 4, steps = (p.Kdim + 31) / 32;
+  const __amdgpu_buffer_rsrc_t rX = make_rsrc(p.A, (uint32_t)p.a_bytes);
+  const uint32_t ldb2 = (uint32_t)p.ldb * 2u;
+  const __amdgpu_buffer_rsrc_t rW = make_rsrc(reinterpret_cast<const bf16_t*>(p.B) + ((int64_t)g * p.b_goff + p.b_off),
+                                              (uint32_t)(p.Kdim - 1) * ldb2 + (uint32_t)(p.up + p.half) * 2u);
+  const int col = h0 + NCL * c16;
+  const uint32_t g_off = col < p.half ? (uint32_t)(8 * kg) * ldb2 + (uint32_t)col * 2u : OOB;
+  const uint32_t u_off = col < p.half ? g_off + (uint32_t)p.up * 2u : OOB;
+  int entry[RG];                                    // of the row map; asked for first, waited for behind the weights' requests
+#pragma unroll
+  for (int q = 0; q < RG; ++q) {
+    entry[q] = lo + min(m0 + 16 * q + c16, n - 1);
+    if (p.gather != nullptr) entry[q] = p.gather[entry[q]];
+  }
+  Cols<NCL> wg[PF][8], wu[PF][8];
+  u32x4_t x[PF][RG];
+  uint32_t x_off[RG];
+  auto request_w = [&](int slot, int s) {
+    const bool in = 32 * s + 8 * kg < p.Kdim;       // K is a multiple of 8: a lane's 8 k exist together
+    const int at = min(s, steps - 1);
+    const uint32_t og = in ? g_off : OOB, ou = in ? u_off : OOB;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      wg[slot][j].load(rW, og, (uint32_t)(32 * at + j) * ldb2);
+      wu[slot][j].load(rW, ou, (uint32_t)(32 * at + j) * ldb2);
+    }
+  };
+  auto request_x = [&](int slot, int s) {
+    const bool in = 32 * s + 8 * kg < p.Kdim;
+#pragma unroll
+    for (int q = 0; q < RG; ++q) x[slot][q] = __builtin_amdgcn_raw_buffer_load_b128(rX, (int)(in ? x_off[q] : OOB), 64 * min(s, steps - 1), 0);
+  };
+  f32x4_t ag[RG][NCL], au[RG][NCL];
+#pragma unroll
+  for (int q = 0; q < RG; ++q)
+#pragma unroll
+    for (int i = 0; i < NCL; ++i) ag[q][i] = au[q][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int u = 0; u < PF; ++u) {
+    request_w(u, wave + WAVES * u);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int q = 0; q < RG; ++q) {
+    int row = m0 + 16 * q + c16 < n ? entry[q] : -1;
+    if (p.gather != nullptr && row >= 0) row = token(p, row);
+    x_off[q] = row >= 0 ? (uint32_t)row * (uint32_t)p.lda * 2u + (uint32_t)kg * 16u : OOB;
+  }
+#pragma unroll
+  for (int u = 0; u < PF; ++u) {
+    request_x(u, wave + WAVES * u);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  for (int s0 = wave; s0 < steps; s0 += WAVES * PF) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+#pragma unroll
+      for (int i = 0; i < NCL; ++i) {
+        Frag fg, fu;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          const uint32_t sel = (i & 1) ? 0x07060302u : 0x05040100u;
+          fg.q[d] = __builtin_amdgcn_perm(wg[u][2 * d + 1].pair(i / 2), wg[u][2 * d].pair(i / 2), sel);
+          fu.q[d] = __builtin_amdgcn_perm(wu[u][2 * d + 1].pair(i / 2), wu[u][2 * d].pair(i / 2), sel);
+        }
+#pragma unroll
+        for (int q = 0; q < RG; ++q) {
+          Frag fx;
+          fx.q = x[u][q];
+          ag[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx.v, fg.v, ag[q][i], 0, 0, 0);
+          au[q][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx.v, fu.v, au[q][i], 0, 0, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      request_w(u, s0 + WAVES * (u + PF));
+      request_x(u, s0 + WAVES * (u + PF));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < RG; ++q) {
+    if (m0 + 16 * q >= n) break;                    // (uniform)
+    float2 gs[UNITS], us[UNITS];
+    auto meet = [&](const f32x4_t (&acc)[NCL], float2 (&sum)[UNITS]) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NCL; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) red[(wave * 16 + 4 * kg + r) * PITCH + NCL * c16 + i] = acc[i][r];
+      __syncthreads();
+#pragma unroll
+      for (int v = 0; v < UNITS; ++v) {
+        const int at = tid + 64 * WAVES * v, row = at / (TH / 2), c = at % (TH / 2) * 2;
+        sum[v] = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int t = 0; t < WAVES; ++t) {
+          const float2 a = *reinterpret_cast<const float2*>(&red[(t * 16 + row) * PITCH + c]);
+          sum[v].x += a.x;
+          sum[v].y += a.y;
+        }
+      }
+    };
+    meet(ag[q], gs);
+    meet(au[q], us);
+    with_act(p.act, [&](auto act) {
+      constexpr int ACT = decltype(act)::value;
+#pragma unroll
+      for (int v = 0; v < UNITS; ++v) {
+        const int at = tid + 64 * WAVES * v, row = m0 + 16 * q + at / (TH / 2), c = h0 + at % (TH / 2) * 2;
+        if (row < n && c < p.half)
+          store_pair(p, lo + row, c, make_float2(gate_value<ACT, true>(gs[v].x) * us[v].x, gate_value<ACT, true>(gs[v].y) * us[v].y));
+      }
+    });
+  }
+}
+
 // RG: groups of 16 rows that go along with one reading of the weights; an expert with more rows takes another one.
 constexpr int FIRST_WAVES = 8, SECOND_WAVES = 4;
 template <int NCL, int RG>
@@ -160,6 +284,18 @@ __global__ __launch_bounds__(64 * FIRST_WAVES) void ragged_few_first(const FewAr
     few_rows<NCL, RG, FIRST_WAVES>(p, red, g, lo, n, m0, n0, 0, (p.Kdim + 31) / 32, [&](int row, int col, const float2& v) {
       store_pair(p, row, col, make_float2(gelu_fast(v.x), gelu_fast(v.y)));
     });
+}
+
+template <int NCL, int RG, int WAVES, int PF>
+__global__ __launch_bounds__(64 * WAVES, 2) void ragged_few_glu(const FewArgs p) {
+  __shared__ float red[few_floats<NCL, WAVES>()];
+  const int cleared = (int)blockIdx.x * 64 * WAVES + (int)threadIdx.x;
+  if (cleared < p.n_arrived) p.arrived[cleared] = 0;
+  const int tile = (int)blockIdx.x;
+  if (tile >= p.total_tiles) return;
+  const int g = tile / p.tiles_n, h0 = (tile - g * p.tiles_n) * 16 * NCL;
+  const int lo = __builtin_amdgcn_readfirstlane(offset(p, g)), n = __builtin_amdgcn_readfirstlane(offset(p, g + 1)) - lo;
+  for (int m0 = 0; m0 < n; m0 += 16 * RG) few_rows_glu<NCL, RG, WAVES, PF>(p, red, g, lo, n, m0, h0);
 }
 
 template <int RG>
@@ -233,7 +369,7 @@ size_t few_rows_bytes(int64_t R, int E, int M, int Hl) {
   return align_up((size_t)E * ((M + 127) / 128) * 4, 256) + align_up((size_t)second_parts(M, Hl) * R * M * 4, 256);
 }
 
-void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, void* ws, hipStream_t st) {
+void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, bool gated, void* ws, hipStream_t st) {
   FewArgs a{}, y{};
   static_cast<RaggedArgs&>(a) = first;
   static_cast<RaggedArgs&>(y) = second;
@@ -254,6 +390,28 @@ void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, void* ws
     const int grid = std::max(a.total_tiles, (a.n_arrived + 64 * FIRST_WAVES - 1) / (64 * FIRST_WAVES));
     hipLaunchKernelGGL((ragged_few_first<NCL, RG>), dim3((unsigned)grid), dim3(64 * FIRST_WAVES), 0, st, a);
   };
+  auto launch_glu = [&](auto ncl, auto rg, auto waves, auto pf) {
+    constexpr int NCL = decltype(ncl)::value, WAVES = decltype(waves)::value;
+    a.tiles_n = (a.half + 16 * NCL - 1) / (16 * NCL);
+    a.total_tiles = a.G * a.tiles_n;
+    const int grid = std::max(a.total_tiles, (a.n_arrived + 64 * WAVES - 1) / (64 * WAVES));
+    hipLaunchKernelGGL((ragged_few_glu<NCL, decltype(rg)::value, WAVES, decltype(pf)::value>), dim3((unsigned)grid), dim3(64 * WAVES), 0, st, a);
+  };
+  if (gated) {
+    // wide rows of the weights where there are enough of them for the chip: 64 rows, 8 experts x 4096 x 14336, 128 and 64 hidden columns a workgroup, 509
+    // and 521 us the whole call; 2 rows, 8 x 1024 x 4096 23 and 20
+    const int64_t wide = std::min<int64_t>(a.R, a.G) * ((a.half + 127) / 128);
+    with_groups([&](auto rg) {
+      if constexpr (decltype(rg)::value == 1) {
+        if (wide >= num_cus()) launch_glu(integral_constant<int, 8>{}, rg, integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        else launch_glu(integral_constant<int, 4>{}, rg, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+      } else {
+        launch_glu(integral_constant<int, 4>{}, rg, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+      }
+      hipLaunchKernelGGL((ragged_few_second<decltype(rg)::value>), dim3(FEW_GRID), dim3(64 * SECOND_WAVES), 0, st, y);
+    });
+    return;
+  }
   const int64_t tiles128 = std::min<int64_t>(a.R, a.G) * ((a.Ndim + 127) / 128);
   with_groups([&](auto rg) {
     if (tiles128 >= num_cus()) launch(integral_constant<int, 8>{}, rg);
