@@ -4,8 +4,8 @@
 //   along rows      a lane takes 8 columns, four neighbouring lanes hold a block, and 64 lanes hold the 512 columns whose scales lie together: the
 //                   four bytes of a dword meet by two exchanges.
 //   along columns   (a weight [K, N] is summed over K)  a lane takes two columns and reads their 32 values of a block from 32 rows, a
-//                   wave 256 (512) bytes of each; nothing is exchanged.  The four waves of a workgroup take a quarter of a chunk each, so
-//                   that a column's 64 bytes are written by one wave, and its scales meet in LDS.
+//                   wave 256 (512) bytes of each; nothing is exchanged.  The four waves of a workgroup take a quarter of a chunk each; the chunk's
+//                   256 bytes of each column meet in LDS and are written (read) as whole lines, and so are its scales.
 #include <algorithm>
 
 #include "mx4.h"
@@ -113,17 +113,18 @@ __global__ __launch_bounds__(MX4_THREADS) void mx4_rows_load(const uint8_t* __re
 
 // ---- blocks along columns: n columns, K rows ----
 constexpr int COLS = 128;      // columns of a workgroup
+constexpr int COL_PITCH = MX4_CHUNK / 2 + 16;      // bytes of a column's chunk in LDS
 template <typename T>
 __global__ __launch_bounds__(MX4_THREADS) void mx4_cols_store(const T* __restrict__ x, const Mx4Shape sh, int64_t groups, uint8_t* __restrict__ q,
                                                               uint32_t* __restrict__ s) {
   using Two = typename Values<T>::Two;
-  __shared__ uint8_t bytes[4][COLS][4];      // [q][column][s]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ __attribute__((aligned(16))) uint8_t codes[COLS * COL_PITCH];
+  __shared__ __attribute__((aligned(4))) uint8_t bytes[4][COLS][4];      // [q][column][s]
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t unit = blockIdx.x, g = unit / (groups * sh.chunks), rest = unit - g * groups * sh.chunks;
   const int c = (int)(rest / groups);
   const int64_t c0 = (rest - c * groups) * COLS, col = c0 + 2 * lane;
-  const bool here = col < sh.n;
-  const T* from = x + g * sh.n * sh.K + (here ? col : 0);
+  const T* from = x + g * sh.n * sh.K + (col < sh.n ? col : 0);
   Two in[2][MX4_BLOCK];
   auto fetch = [&](int i, Two (&d)[MX4_BLOCK]) {      // rows behind the last one: that one, zeroed below
     const int k0 = (c * 16 + 4 * wave + i) * MX4_BLOCK;
@@ -134,9 +135,7 @@ __global__ __launch_bounds__(MX4_THREADS) void mx4_cols_store(const T* __restric
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (i < 3) fetch(i + 1, in[(i + 1) & 1]);
-    const int block = c * 16 + 4 * wave + i, left = sh.K - block * MX4_BLOCK;
-    uint4 out[2];
-    int b[2];
+    const int left = sh.K - (c * 16 + 4 * wave + i) * MX4_BLOCK;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       float v[MX4_BLOCK];
@@ -147,50 +146,72 @@ __global__ __launch_bounds__(MX4_THREADS) void mx4_cols_store(const T* __restric
         v[k] = k < left ? (h ? f.y : f.x) : 0.f;
         top = max(top, __float_as_uint(v[k]) & 0x7FFFFFFFu);
       }
-      b[h] = left > 0 ? mx4_scale(top) : 0;
+      const int b = left > 0 ? mx4_scale(top) : 0;
       uint32_t w[4];
 #pragma unroll
       for (int d = 0; d < 4; ++d) {
         float t[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) t[e] = v[8 * d + e];
-        w[d] = mx4_pack(t, b[h]);
+        w[d] = mx4_pack(t, b);
       }
-      out[h] = make_uint4(w[0], w[1], w[2], w[3]);
-      bytes[i][2 * lane + h][wave] = (uint8_t)b[h];
-    }
-    if (here && left > 0) {
-      uint4* to = reinterpret_cast<uint4*>(q + ((g * sh.n + col) * sh.blocks + block) * 16);
-      to[0] = out[0];
-      to[sh.blocks] = out[1];
+      *reinterpret_cast<uint4*>(codes + (2 * lane + h) * COL_PITCH + (4 * wave + i) * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+      bytes[i][2 * lane + h][wave] = (uint8_t)b;
     }
   }
   __syncthreads();
+  const int blocks = min(16, sh.blocks - c * 16);     // of this chunk
 #pragma unroll
-  for (int u = threadIdx.x; u < 4 * COLS; u += MX4_THREADS) {
+  for (int u = tid; u < COLS * 16; u += MX4_THREADS) {
+    const int k = u / 16, block = u % 16;
+    if (c0 + k < sh.n && block < blocks)
+      *reinterpret_cast<uint4*>(q + ((g * sh.n + c0 + k) * sh.blocks + c * 16 + block) * 16) = *reinterpret_cast<const uint4*>(codes + k * COL_PITCH + block * 16);
+  }
+#pragma unroll
+  for (int u = tid; u < 4 * COLS; u += MX4_THREADS) {
     const int i = u / COLS, k = u % COLS;
     if (c0 + k < sh.n) s[((g * sh.chunks + c) * 4 + i) * sh.n + c0 + k] = *reinterpret_cast<const uint32_t*>(bytes[i][k]);
   }
 }
 
 template <typename T>
-__global__ __launch_bounds__(MX4_THREADS) void mx4_cols_load(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, const Mx4Shape sh,
+__global__ __launch_bounds__(MX4_THREADS) void mx4_cols_load(const uint8_t* __restrict__ q, const uint32_t* __restrict__ s, const Mx4Shape sh,
                                                              int64_t groups, T* __restrict__ x) {
   using Two = typename Values<T>::Two;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ __attribute__((aligned(16))) uint8_t codes[COLS * COL_PITCH];
+  __shared__ __attribute__((aligned(4))) uint8_t bytes[4][COLS][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t unit = blockIdx.x, g = unit / (groups * sh.chunks), rest = unit - g * groups * sh.chunks;
   const int c = (int)(rest / groups);
-  const int64_t col = (rest - c * groups) * COLS + 2 * lane;
+  const int64_t c0 = (rest - c * groups) * COLS, col = c0 + 2 * lane;
+  const int blocks = min(16, sh.blocks - c * 16);
+  uint4 in[COLS * 16 / MX4_THREADS];
+#pragma unroll
+  for (int r = 0; r < COLS * 16 / MX4_THREADS; ++r) {
+    const int u = tid + r * MX4_THREADS, k = u / 16, block = u % 16;
+    in[r] = make_uint4(0, 0, 0, 0);
+    if (c0 + k < sh.n && block < blocks) in[r] = *reinterpret_cast<const uint4*>(q + ((g * sh.n + c0 + k) * sh.blocks + c * 16 + block) * 16);
+  }
+#pragma unroll
+  for (int u = tid; u < 4 * COLS; u += MX4_THREADS) {
+    const int i = u / COLS, k = u % COLS;
+    if (c0 + k < sh.n) *reinterpret_cast<uint32_t*>(bytes[i][k]) = s[((g * sh.chunks + c) * 4 + i) * sh.n + c0 + k];
+  }
+#pragma unroll
+  for (int r = 0; r < COLS * 16 / MX4_THREADS; ++r) {
+    const int u = tid + r * MX4_THREADS;
+    *reinterpret_cast<uint4*>(codes + u / 16 * COL_PITCH + u % 16 * 16) = in[r];
+  }
+  __syncthreads();
   if (col >= sh.n) return;
   T* to = x + g * sh.n * sh.K + col;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int block = c * 16 + 4 * wave + i, left = sh.K - block * MX4_BLOCK;
+    const int block = 4 * wave + i, k0 = (c * 16 + block) * MX4_BLOCK, left = sh.K - k0;
     if (left <= 0) break;
-    const uint4* from = reinterpret_cast<const uint4*>(q + ((g * sh.n + col) * sh.blocks + block) * 16);
-    const uint4 a = from[0], d = from[sh.blocks];
-    const uint8_t* sb = s + (((g * sh.chunks + c) * 4 + i) * sh.n + col) * 4 + wave;
-    const int ba = sb[0], bd = sb[4];
+    const uint4 a = *reinterpret_cast<const uint4*>(codes + 2 * lane * COL_PITCH + block * 16);
+    const uint4 d = *reinterpret_cast<const uint4*>(codes + (2 * lane + 1) * COL_PITCH + block * 16);
+    const int ba = bytes[i][2 * lane][wave], bd = bytes[i][2 * lane + 1][wave];
     const uint32_t wa[4] = {a.x, a.y, a.z, a.w}, wd[4] = {d.x, d.y, d.z, d.w};
 #pragma unroll
     for (int p = 0; p < 4; ++p) {
@@ -199,7 +220,7 @@ __global__ __launch_bounds__(MX4_THREADS) void mx4_cols_load(const uint8_t* __re
       mx4_values(wd[p], bd, vd);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (8 * p + e < left) *reinterpret_cast<Two*>(to + (int64_t)(block * MX4_BLOCK + 8 * p + e) * sh.n) = Values<T>::put(va[e], vd[e]);
+        if (8 * p + e < left) *reinterpret_cast<Two*>(to + (int64_t)(k0 + 8 * p + e) * sh.n) = Values<T>::put(va[e], vd[e]);
     }
   }
 }
@@ -248,7 +269,7 @@ template <typename T>
 void load_cols(const void* q, const void* s, int64_t G, int rows, int64_t cols, void* x, hipStream_t st) {
   const Mx4Shape sh = shape_of(cols, rows);
   const int64_t groups = (cols + COLS - 1) / COLS;
-  hipLaunchKernelGGL((mx4_cols_load<T>), dim3((unsigned)(G * sh.chunks * groups)), dim3(MX4_THREADS), 0, st, (const uint8_t*)q, (const uint8_t*)s, sh, groups,
+  hipLaunchKernelGGL((mx4_cols_load<T>), dim3((unsigned)(G * sh.chunks * groups)), dim3(MX4_THREADS), 0, st, (const uint8_t*)q, (const uint32_t*)s, sh, groups,
                      (T*)x);
 }
 

@@ -398,13 +398,13 @@ void launch_few_rows(const RaggedArgs& first, const RaggedArgs& second, bool gat
     hipLaunchKernelGGL((ragged_few_glu<NCL, decltype(rg)::value, WAVES, decltype(pf)::value>), dim3((unsigned)grid), dim3(64 * WAVES), 0, st, a);
   };
   if (gated) {
-    // wide rows of the weights where there are enough of them for the chip: 64 rows, 8 experts x 4096 x 14336, 128 and 64 hidden columns a workgroup, 509
-    // and 521 us the whole call; 2 rows, 8 x 1024 x 4096 23 and 20
+    // Wide rows of the weights where there are enough of them for the chip.  128 and 64 hidden columns a workgroup, the whole call: 64 rows, 8 experts x
+    // 4096 x 14336 509 and 515 us, 2 rows 131 and 144; 8 rows, 8 x 1024 x 4096 35.1 and 38.8; but 2 rows, 8 x 2048 x 8192 50.4 and 45.1.  32 columns gain nothing.
     const int64_t wide = std::min<int64_t>(a.R, a.G) * ((a.half + 127) / 128);
     with_groups([&](auto rg) {
       if constexpr (decltype(rg)::value == 1) {
-        if (wide >= num_cus()) launch_glu(integral_constant<int, 8>{}, rg, integral_constant<int, 8>{}, integral_constant<int, 1>{});
-        else launch_glu(integral_constant<int, 4>{}, rg, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+        if (4 * wide >= 3 * num_cus()) launch_glu(integral_constant<int, 8>{}, rg, integral_constant<int, 8>{}, integral_constant<int, 1>{});
+        else launch_glu(integral_constant<int, 4>{}, rg, integral_constant<int, 8>{}, integral_constant<int, 2>{});
       } else {
         launch_glu(integral_constant<int, 4>{}, rg, integral_constant<int, 4>{}, integral_constant<int, 2>{});
       }
