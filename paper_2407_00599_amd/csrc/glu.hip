@@ -185,6 +185,9 @@ __global__ __launch_bounds__(64 * CF::NW) void glu_gemm_dma(const RaggedArgs p) 
   gemm_dma_tile<KIND, EPI, CF, ROWS_PLAIN, Glu>(p, smem, (int)blockIdx.x);
 }
 
+using Tile256Brief = TileCfg<256, 256, 2, 4, 1, 3, 2, 32>;
+constexpr int BRIEF_ROWS = 4096;      // of an expert, on average
+
 // dX, dW2 and the gate's and the up projection's half of dW1, which only depend on dG, dU and A', in one launch; the last two read X's rows
 template <typename CFX, typename CFW, int EPI>
 __global__ __launch_bounds__(512) void glu_bwd_quad(const RaggedArgs px, const RaggedArgs pw2, const RaggedArgs pwg, const RaggedArgs pwu, int nbx, int nb2,
@@ -255,11 +258,15 @@ void launch_glu_backward(RaggedArgs dx, RaggedArgs w2, RaggedArgs wg, RaggedArgs
       if (w2.splits > 1) launch(Tile64x128{}, Tile128{}, std::integral_constant<int, EPI_PART>{});
       else launch(Tile64x128{}, Tile128{}, Store{});
     } else {
+      // A compute unit holds one workgroup of this launch whatever its tile (the LDS of a 256 x 256 one), so the tile of 192 rows gains nothing.  Weight
+      // gradients of few k tiles are not under the power limit and take 32 x 32 x 16 instructions.  dX in tiles of 192 and 256 rows, and those: 8 experts of 1024
+      // rows x 1024 x 4096 475, 437 and 432 us, 2 of 2048 x 2048 x 8192 728, 666 and 650; 1 of 32768 x 1024 x 2816 1414, 1347 and 1362.
       const TilePlan t = plan_rows(dx, true);
-      if (t.tile_m == 256) launch(Tile256{}, Tile256{}, Store{});
-      else if (t.tile_m == 192) launch(Tile192{}, Tile256{}, Store{});
-      else if (t.tile_m == 128) launch(Tile128{}, Tile256{}, Store{});
-      else launch(Tile64x128{}, Tile256{}, Store{});
+      const bool brief = dx.R <= BRIEF_ROWS * (int64_t)dx.G;
+      if (t.tile_m >= 192 && !brief) launch(Tile256{}, Tile256{}, Store{});
+      else if (t.tile_m >= 192) launch(Tile256{}, Tile256Brief{}, Store{});
+      else if (t.tile_m == 128) launch(Tile128{}, Tile256Brief{}, Store{});
+      else launch(Tile64x128{}, Tile256Brief{}, Store{});
     }
   }
   if (w2.splits > 1) {

@@ -65,7 +65,8 @@ LARGE = [
     ((130, 257, 5, 0), 200, 1040, 2064, 1, 0, True),         # 64 x 128, 64 x 128
     # the merged backward launch with dX in these tiles beside weight gradients of 256 x 256
     ((900, 1200, 0, 900), 10, 4104, 72, 1, 0, True),         # 256 x 256
-    ((1300, 2, 500, 190), 8, 4104, 144, 2, 1, True),         # 192 x 256, a shard
+    ((1300, 2, 500, 190), 8, 4104, 144, 2, 1, True),         # 256 x 256, a shard
+    ((5000, 4200, 4100, 3300), 8, 4104, 72, 1, 0, False),    # 256 x 256, weight gradients of many k tiles
     ((300, 0, 0, 695), 5, 4104, 72, 1, 0, False),            # 128 x 128
 ]
 
