@@ -340,6 +340,16 @@ def _typed(dtype, *tensors):
             raise ValueError(f"expected {dtype}, got {t.dtype}")
 
 
+def _here(*tensors):
+    """A call goes to the current device's stream: tensors of another one, or of the host, are refused."""
+    if not all(t is None or t.is_cuda for t in tensors):
+        raise ValueError("tensors must live on the GPU")
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"tensors must live on the current device, cuda:{device}: got one on {t.device}")
+
+
 def moe_ragged_plan(idx, slot, counts, S, E, k, C, offsets, row_idx, row_slot, row_inv):
     _typed(torch.int32, idx, slot, counts, offsets, row_idx, row_slot, row_inv)
     _check((_lib or lib()).moe_ragged_plan(_ptr(idx), _ptr(slot), _ptr(counts), S, E, k, C, _ptr(offsets), _ptr(row_idx),
@@ -397,6 +407,7 @@ def moe_ragged_glu_workspace_bytes(dtype, R, E, M, H, n_esp, backward) -> int:
 
 
 def moe_ragged_glu_fwd(x, S, inv, k, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, act, Z, A, Y, ws=None):
+    _here(x, inv, W1, W2, offsets, Z, A, Y, ws)
     wp, wb = _ws_args(ws)
     _typed(torch.int32, inv, offsets)
     _check((_lib or lib()).moe_ragged_glu_fwd(_ptr(x), _same_dtype(x, W1, W2, A, Y, *([] if Z is None else [Z])), S, _ptr(inv), k, _ptr(W1),
@@ -405,6 +416,7 @@ def moe_ragged_glu_fwd(x, S, inv, k, W1, W2, offsets, R, E, M, H, esp_idx, n_esp
 
 
 def moe_ragged_glu_bwd(dY, x, S, inv, k, Z, W1, W2, offsets, R, E, M, H, esp_idx, n_esp, act, dX, dW1, dW2, ws):
+    _here(dY, x, inv, Z, W1, W2, offsets, dX, dW1, dW2, ws)
     wp, wb = _ws_args(ws)
     _typed(torch.int32, inv, offsets)
     _check((_lib or lib()).moe_ragged_glu_bwd(_ptr(dY), _ptr(x), _same_dtype(x, dY, Z, W1, W2, dX, dW1, dW2), S, _ptr(inv), k, _ptr(Z),
@@ -433,12 +445,14 @@ def mx4_shapes(G, rows, cols, transposed):
 
 
 def moe_mx4_store(x, G, rows, cols, transposed, q, scales):
+    _here(x, q, scales)
     _typed(torch.uint8, q, scales)
     _check((_lib or lib()).moe_mx4_store(_ptr(x), dtype_code(x), G, rows, cols, int(transposed), _ptr(q), _ptr(scales), _stream()),
            "moe_mx4_store")
 
 
 def moe_mx4_load(q, scales, G, rows, cols, transposed, x):
+    _here(q, scales, x)
     _typed(torch.uint8, q, scales)
     _check((_lib or lib()).moe_mx4_load(_ptr(q), _ptr(scales), G, rows, cols, int(transposed), _ptr(x), dtype_code(x), _stream()),
            "moe_mx4_load")
@@ -449,6 +463,7 @@ def moe_ragged_gemm_mx4_workspace_bytes(R, E, K, N) -> int:
 
 
 def moe_ragged_gemm_mx4(xq, xs, S, inv, k, Wq, Ws, offsets, R, E, K, N, Y, ws=None):
+    _here(xq, xs, inv, Wq, Ws, offsets, Y, ws)
     wp, wb = _ws_args(ws)
     _typed(torch.int32, inv, offsets)
     _typed(torch.uint8, xq, xs, Wq, Ws)
@@ -461,6 +476,7 @@ def moe_ragged_glu_mx4_workspace_bytes(S, R, E, M, H) -> int:
 
 
 def moe_ragged_glu_mx4(x, S, inv, k, W1q, W1s, W2q, W2s, offsets, R, E, M, H, act, Y, ws):
+    _here(x, inv, W1q, W1s, W2q, W2s, offsets, Y, ws)
     wp, wb = _ws_args(ws)
     _typed(torch.int32, inv, offsets)
     _typed(torch.uint8, W1q, W1s, W2q, W2s)

@@ -55,6 +55,13 @@ SIZES = [
     ((1,), 0, 512, 2048, 1, 0, True), ((0, 3, 0, 0, 1, 0, 7, 0), 3, 520, 2200, 1, 0, True), ((40, 0, 1, 0, 2, 0, 0), 5, 512, 4160, 2, 1, True),
     ((20,), 2, 264, 4096, 1, 0, False), ((0,) * 65 + (3, 0, 2), 1, 136, 8200, 1, 0, True),
 ]
+# few rows of large experts (bf16), in the kernels for them
+FEW = [
+    ((3, 0, 9, 1, 0, 2, 17, 4), 5, 264, 4096, 1, 0, True),   # 128 hidden columns a workgroup, an expert with more rows than go along with one reading
+    ((5, 20, 0), 2, 520, 5400, 1, 0, True),                  # 64 hidden columns
+    ((20, 9), 1, 520, 16400, 2, 1, False),                   # two groups of rows, a shard, rows as they lie
+    ((0, 0, 31, 1), 0, 1032, 2072, 1, 0, True),
+]
 # the tiles of large problems (bf16), each around the smallest size for which the dispatch chooses it
 LARGE = [
     ((700, 0, 830), 20, 72, 4104, 1, 0, True),               # forward 256 x 256, gradients of g and u 128 x 128
@@ -139,6 +146,16 @@ def run(size, dtype, act):
 @pytest.mark.parametrize("size", SIZES, ids=lambda s: f"{sum(s[0])}x{s[2]}x{s[3]}")
 def test_glu(size, dtype, act):
     run(size, dtype, act)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("size", FEW, ids=lambda s: f"{sum(s[0])}x{s[2]}x{s[3]}")
+def test_glu_of_few_rows(size, act):
+    ns, behind, M, H, n_esp = size[:5]
+    R, E = sum(ns) + behind, len(ns)
+    tiles = api.moe_ragged_glu_workspace_bytes(api.MOE_BF16, 65, E, M, H, n_esp, 0)      # no parts in bf16
+    assert api.moe_ragged_glu_workspace_bytes(api.MOE_BF16, R, E, M, H, n_esp, 0) > tiles == 0
+    run(size, "bf16", act)
 
 
 @pytest.mark.parametrize("size", LARGE, ids=lambda s: f"{sum(s[0])}x{s[2]}x{s[3]}")

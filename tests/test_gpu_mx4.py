@@ -2,12 +2,13 @@
 element by element.
 
 Bounds.  Products of two 4-bit values are exact; a sum of K of them carries at most K 2^-23 of the sum of magnitudes in fp32, as in test_gpu_ragged.py.  Of
-the FFN's hidden values, which are known to some bound, 4 bits keep anything between what the ends of that range are kept as (O.kept_range); beyond
+the FFN's hidden values, which are known to some bound, 4 bits keep anything between what the ends of that range are kept as (four_bits.kept_range); beyond
 that its second product is one of exact values."""
 import numpy as np
 import pytest
 import torch
 
+import four_bits as F
 from oracle import mx4_oracle as O
 from oracle import ragged_oracle as RO
 from paper_2407_00599_amd import api
@@ -86,7 +87,7 @@ class Four:
         rows = c.S if gather else c.R
         c.x[::3] *= 16
         self.xq, self.xs = store(c.x.view(1, rows, K), False)
-        kept = O.kept(host(c.x))
+        kept = F.kept(host(c.x))
         self.X = RO.rows_of(kept, host(c.inv), c.k) if gather else kept.copy()
         self.rows = rows
 
@@ -94,7 +95,7 @@ class Four:
         """bytes and what they stand for, [E, K, N]"""
         W = self.c.stored(self.c.rng.standard_normal((self.c.E, K, N)) * gain / np.sqrt(K))
         q, s = store(W, True)
-        return q, s, np.stack([O.kept(host(w).T).T for w in W])
+        return q, s, np.stack([F.kept(host(w).T).T for w in W])
 
 
 # rows per expert, rows behind, K, N, gather
@@ -145,8 +146,8 @@ def test_glu(ns, behind, M, H, gather, dtype, act):
     a = O.glu(f.X, wg, wu, act, off)
     ea = act_bounds(act, "f32", np.abs(G) + dG)[0] + 1.13 * dG
     d = ea * (np.abs(U) + dU) + np.abs(RO.gate_act(act, G)[0]) * dU + 2.0 ** -23 * np.abs(a)
-    lo, hi = O.kept_range(a, d)
-    kept = O.kept(a)
+    lo, hi = F.kept_range(a, d)
+    kept = F.kept(a)
     spread = np.maximum(hi - kept, kept - lo)
     ref = RO.gemm(kept, W2, off)
     b = RO.gemm(spread, np.abs(W2), off) + c.sums(H) * RO.gemm(np.abs(kept) + spread, np.abs(W2), off)
@@ -213,3 +214,18 @@ def test_same_bits_again_from_a_graph_and_on_another_stream():
         assert torch.equal(Y, ref)
         step()
         torch.cuda.synchronize()
+
+
+def test_tensors_elsewhere_are_refused(monkeypatch):
+    """A call goes to the current device's stream: its tensors have to live there."""
+    x = torch.zeros(1, 8, 64, device=DEV)
+    q, s = (torch.zeros(shape, dtype=torch.uint8, device=DEV) for shape in api.mx4_shapes(1, 8, 64, False))
+    for bad in ((x.cpu(), q, s), (x, q.cpu(), s), (x, q, s.cpu())):
+        with pytest.raises(ValueError):
+            api.moe_mx4_store(bad[0], 1, 8, 64, False, bad[1], bad[2])
+    for bad in ((x.half(), q, s), (x, q.char(), s), (x, q, s.int()), (x.transpose(1, 2), q, s)):
+        with pytest.raises(ValueError):
+            api.moe_mx4_store(bad[0], 1, 8, 64, False, bad[1], bad[2])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device"):
+        api.moe_mx4_store(x, 1, 8, 64, False, q, s)
