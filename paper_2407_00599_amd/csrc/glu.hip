@@ -8,6 +8,11 @@
 // interleaving is in the addresses of the requests alone (Glu::column): 256 tile columns are 256 bytes of either half of a row of W1, whole lines.
 // dX is one product over 2 H_l: of a shard the second half's k indexes lie elsewhere in W1 (Glu::k_skip).
 // In bf16, A, A', dG and dU are rounded between two products, as in the FFN with one projection.
+//
+// Bound by the matrix instructions in training and by reading the weights in serving.  bf16, us of the launches: 4096 tokens top-2 of 8 experts x 1024 x 4096
+// (16 k tiles a tile, so what is outside the k loop weighs: a third) first product with Z kept 187 (0.74 PFLOP/s), A W2 91, dA and its epilogue 129, dX and the
+// weight gradients 407 (0.84); 16384 tokens top-2 of 8 experts x 4096 x half of 14336, under the power limit, 3018, 1571, 1752 and 8077 (1.2 to 1.28 PFLOP/s
+// where the launch is a product alone); 256 tokens top-2 of 8 experts x 4096 x 14336, A kept alone, 425 and 208 (4.4 and 4.5 TB/s of weights).
 #include "ragged_tile.h"
 
 namespace moe {

@@ -1,6 +1,7 @@
 // A tensor to microscaled 4-bit floating point (mx4.h) and back, with the blocks along its rows or along its columns.
 //
-// Bound by memory: 2 (4) + 17/32 bytes a value in bf16 (fp32), each direction.
+// Bound by memory: 2 (4) + 17/32 bytes a value in bf16 (fp32), each direction.  Along columns, bf16, 8 x 4096 x 28672 508 us to 4 bits (4.7 TB/s) and
+// 447 back (5.3); along rows, bf16, 16384 x 4096 44 us (3.9 TB/s), fp32 of 1003 x 1544 4.2 and 4.5, the latency of one read and one write.
 //   along rows      a lane takes 8 columns, four neighbouring lanes hold a block, and 64 lanes hold the 512 columns whose scales lie together: the
 //                   four bytes of a dword meet by two exchanges.
 //   along columns   (a weight [K, N] is summed over K)  a lane takes two columns and reads their 32 values of a block from 32 rows, a

@@ -308,6 +308,20 @@ class DroplessBlock:
             nbytes += [api.moe_gate_bwd_workspace_bytes(S, M, E), api.moe_norm_bwd_workspace_bytes(S, M), ffn_bytes(self.code, R, E, M, H, 1, 1)]
         self.ws = torch.empty(max(nbytes), dtype=torch.uint8, device=device)
 
+    def gated_sizes(self):
+        return ("W1", self.M, 2 * self.H), ("W2", self.H, self.M)
+
+    def _check_gated(self, p):
+        """W1 of experts with one projection, or of another block, would be read beyond its end."""
+        for name, rows, cols in self.gated_sizes():
+            if "W1q" in p:
+                shapes = dict(zip((name + "q", name + "s"), api.mx4_shapes(self.E, rows, cols, True)))
+            else:
+                shapes = {name: (self.E, rows, cols)}
+            for n, shape in shapes.items():
+                if tuple(p[n].shape) != shape:
+                    raise ValueError(f"{n} has the shape {tuple(p[n].shape)}, not {shape}")
+
     def _moe(self, x, p, t, keep):
         """t: where the pass writes."""
         S, M, E, k, R = self.S, self.M, self.E, self.k, self.R
@@ -315,6 +329,8 @@ class DroplessBlock:
         b1, b2 = (p["b1"], p["b2"]) if self.layer else (None, None)
         if not self.layer:
             m1 = m2 = None
+        if self.act is not None:
+            self._check_gated(p)
         api.moe_norm_fwd(x, S, M, self.kind, p["w1"], b1, self.eps, t.u, m1, r1)
         # a token asks for an expert once: capacity S drops nothing
         api.moe_gate_topk(t.u, p["Wg"], None, S, M, E, k, S, 0, 1, self.norm_topk, t.logits, t.idx, t.slot, t.w, self.inv, t.counts, self.ws)
@@ -340,11 +356,10 @@ class DroplessBlock:
         """params for `infer` with the experts' W1 and W2 in 4 bits, 17/32 bytes a weight; the others are the same tensors."""
         if self.act is None:
             raise ValueError('quantise: ffn="swiglu" or "geglu"')
-        p = {n: v for n, v in params.items() if n not in ("W1", "W2")}
-        for name, rows, cols in (("W1", self.M, 2 * self.H), ("W2", self.H, self.M)):
+        p = {n: v for n, v in params.items() if n not in self.MX4 + ("W1", "W2")}
+        self._check_gated({n: params[n] for n in ("W1", "W2")})
+        for name, rows, cols in self.gated_sizes():
             W = params[name]
-            if tuple(W.shape) != (self.E, rows, cols):
-                raise ValueError(f"{name} has the shape {tuple(W.shape)}, not {(self.E, rows, cols)}")
             q, s = (torch.empty(shape, dtype=torch.uint8, device=W.device) for shape in api.mx4_shapes(self.E, rows, cols, True))
             api.moe_mx4_store(W, self.E, rows, cols, True, q, s)
             p[name + "q"], p[name + "s"] = q, s

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2407_00599_amd.api import mx4_shapes
 from paper_2407_00599_amd.layer import DroplessBlock
 
 
@@ -34,3 +35,22 @@ def test_four_bits_only_of_gated_experts_and_only_to_serve():
             gated.quantise(dict(W, **bad))
     with pytest.raises(ValueError):
         gated.quantise(W)                      # tensors must live on the GPU
+
+
+def test_weights_of_other_sizes():
+    """refused in front of the first launch: W1 of experts with one projection, and 4 bits of another block's weights"""
+    gated = DroplessBlock(4, 64, 72, 2, 1, device="cpu", ffn="swiglu")
+    x = torch.zeros(4, 64)
+    good = {"W1": torch.zeros(2, 64, 144), "W2": torch.zeros(2, 72, 64)}
+    for bad in ({"W1": torch.zeros(2, 64, 72)}, {"W2": torch.zeros(2, 64, 72)}, {"W1": torch.zeros(1, 64, 144)}):
+        for call in (gated.forward, gated.infer):
+            with pytest.raises(ValueError, match="has the shape"):
+                call(x, dict(good, **bad))
+    bits = lambda E, M, H: {n + t: torch.zeros(shape, dtype=torch.uint8) for n, rows, cols in (("W1", M, 2 * H), ("W2", H, M))
+                            for t, shape in zip("qs", mx4_shapes(E, rows, cols, True))}
+    for E, M, H in ((2, 64, 64), (2, 32, 72), (1, 64, 72)):
+        with pytest.raises(ValueError, match="has the shape"):
+            gated.infer(x, bits(E, M, H))
+    with pytest.raises((ValueError, KeyError)) as e:       # the right sizes: it is the missing norm weights or the host's tensors
+        gated.infer(x, bits(2, 64, 72))
+    assert "has the shape" not in str(e.value)
