@@ -34,21 +34,29 @@ struct Mx4 : Ragged {
     if constexpr (EPI == EPI_GLU) return min(glu_hidden(n0 + c), p.half - 1) + (((n0 + c) & 16) ? p.half : 0);
     else return min(n0 + c, p.n - 1);
   }
+  // Entry of the row map for row r of an expert (behind its last one: that one's).  Without a map nothing is read, and no branch stands
+  // around the read, so that all of a tile's are requested before the first is waited for (one after the other they took 2 us).
+  static __device__ __forceinline__ int entry(const Args& p, const Place& at, int r) {
+    const __amdgpu_buffer_rsrc_t map = make_rsrc(p.gather, p.gather == nullptr ? 0u : (uint32_t)p.R * 4u);
+    return (int)__builtin_amdgcn_raw_buffer_load_b32(map, (at.lo + min(r, at.n - 1)) * 4, 0, 0);
+  }
+  // row of X that row r of an expert reads, or -1: none
+  static __device__ __forceinline__ int x_row(const Args& p, const Place& at, int r, int entry) {
+    return p.gather == nullptr ? at.lo + min(r, at.n - 1) : token(p, entry);
+  }
   // physical rows as in Ragged::rows; of rows lane, lane + 64 of the wave tile twice the row (+ 1: a row of zeros), or OOB
   template <int TM, int RA>
   static __device__ __forceinline__ void rows(const Args& p, const Place& at, int q0, int w0, int (&q_row)[RA], uint32_t (&out)[2]) {
+    int e[RA + 2];
 #pragma unroll
-    for (int j = 0; j < RA; ++j) q_row[j] = max(x_row(p, at, q0 + 8 * j), 0);
+    for (int j = 0; j < RA + 2; ++j) e[j] = entry(p, at, j < RA ? q0 + 8 * j : w0 + 64 * (j - RA));
+#pragma unroll
+    for (int j = 0; j < RA; ++j) q_row[j] = max(x_row(p, at, q0 + 8 * j, e[j]), 0);
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int r = w0 + 64 * j;
-      if (r < at.n) out[j] = 2u * (uint32_t)(at.lo + r) + (x_row(p, at, r) < 0 ? 1u : 0u);
+      if (r < at.n) out[j] = 2u * (uint32_t)(at.lo + r) + (x_row(p, at, r, e[RA + j]) < 0 ? 1u : 0u);
     }
-  }
-  // row of X that row r of an expert reads, or -1: none; behind the last one any
-  static __device__ __forceinline__ int x_row(const Args& p, const Place& at, int r) {
-    const int row = at.lo + min(r, at.n - 1);
-    return p.gather == nullptr ? row : token(p, p.gather[row]);
   }
 
   template <typename CF>
@@ -73,7 +81,8 @@ struct Mx4 : Ragged {
       plane_b = (uint32_t)p.n * 4u;
       rA = make_rsrc(p.xs, plane_a * 4u * (uint32_t)chunks);
       rB = make_rsrc(p.ws + (int64_t)g * chunks * 16 * p.n, plane_b * 4u * (uint32_t)chunks);
-      off_a = (uint32_t)max(x_row(p, at, at.tm * TM + 64 * (wave % PARTS_A) + lane), 0) * 4u;
+      const int r = at.tm * TM + 64 * (wave % PARTS_A) + lane;
+      off_a = (uint32_t)max(x_row(p, at, r, entry(p, at, r)), 0) * 4u;
       const int c = 64 * (wave % PARTS_B) + lane;
       off_b = (uint32_t)(p.half ? row<EPI_GLU>(p, n0, c) : row<EPI_STORE>(p, n0, c)) * 4u;
       first_a = wave / PARTS_A * PLANES_A;
