@@ -7,9 +7,9 @@
 // the two bytes of its rows for a k tile, which the two steps of the tile select.
 // Tiles have two ring slots for either operand: the scales take the LDS of the third.
 //
-// Bound by power, and with short reductions by what stands outside the k loop: 8 experts of 4096 rows x 4096 x 14336, gated, 2161 us and 935 back (3.56 and
-// 4.12 PFLOP/s; the matrix pipes busy 54 % of the cycles at the 1.6 GHz that the power limit leaves): 1.8 us a k tile of 256 x 256 and 9 us a round
-// of tiles for its first requests and its epilogue, of which storing 33 MB takes 6.  64 experts of 512 rows x 2048 x 2048, 8 k tiles, 139 us (2.0 PFLOP/s).
+// Bound by power, and with short reductions by what stands outside the k loop: 8 experts of 4096 rows x 4096 x 14336, gated, 2110 us and 935 back (3.65 and
+// 4.12 PFLOP/s; the matrix pipes busy 54 % of the cycles at the 1.6 GHz that the power limit leaves): 1.7 to 1.85 us a k tile of 256 x 256 and 8 us a round
+// of tiles, a chain of offsets, row map and first k tile (4 to 7, cold) and the epilogue (2 to 4).  64 experts of 512 rows x 2048 x 2048, 8 k tiles, 139 us (2.0 PFLOP/s).
 // Requests spread over less of the k tile, or over all of it, measured the same; four waves of 128 x 128 spill (486 -> 947 us); tiles of 64 x 128 were nowhere faster.
 #include "mx4_ffn.h"
 
@@ -159,33 +159,41 @@ struct Mx4 : Ragged {
       // pieces of 32 columns are 16 of the gate and 16 of the up projection: two of them are 32 hidden columns, one block of A
       static_assert(NBK == 2, "a wave's hidden columns are one block");
       const int h0 = nbase / 2, block = h0 / MX4_BLOCK;
+      // Nothing stands in a branch, and lane groups meet without LDS: 8 values of a lane go through the exponential and the reciprocal side by side.
+      const bool is[2] = {h0 + 4 * kg < p.half, h0 + 16 + 4 * kg < p.half};
+      const __amdgpu_buffer_rsrc_t rQ = make_rsrc(p.aq, (uint32_t)p.R * (uint32_t)p.a_blocks * 16u),
+                                   rS = make_rsrc(p.as, (uint32_t)p.R * 16u * ((uint32_t)(p.a_blocks + 15) / 16u));
+      const uint32_t q_at = (uint32_t)block * 16u + 8u * (kg & 1) + 4u * (kg >> 1);
+      const uint32_t s_at = (uint32_t)((block >> 4) * 4 + (block & 3)) * (uint32_t)p.R * 4u + (uint32_t)((block >> 2) & 3);
       with_hidden(p.act, p.f32, [&](auto act, auto wide) {
 #pragma unroll
         for (int i = 0; i < AM; ++i) {
           const uint32_t o = row_of(mshift + 16 * i, l16);
-          const bool zero = o == OOB || (o & 1u);
           float v[2][4];
           uint32_t top = 0;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < 2; ++j) {
+            uint32_t t = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float g = acc[i][2 * j][e], u = acc[i][2 * j + 1][e];
-              v[j][e] = zero || h0 + 16 * j + 4 * kg >= p.half ? 0.f : mx4_hidden<decltype(act)::value, decltype(wide)::value>(g, u);
-              top = max(top, __float_as_uint(v[j][e]) & 0x7FFFFFFFu);
+              v[j][e] = mx4_hidden<decltype(act)::value, decltype(wide)::value>(acc[i][2 * j][e], acc[i][2 * j + 1][e]);
+              t = max(t, __float_as_uint(v[j][e]) & 0x7FFFFFFFu);
             }
-          top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
-          top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-          const int b = mx4_scale(top);
-          const uint32_t c0 = mx4_pack4(v[0], b), c1 = mx4_pack4(v[1], b);
-          // neighbouring lane groups make dwords: the even one of columns 0..15, the odd one of 16..31
-          const uint32_t other = (uint32_t)__shfl_xor((int)(kg & 1 ? c0 : c1), 16, 64);
-          const uint32_t four = kg & 1 ? other | c1 << 16 : c0 | other << 16;
-          if (o != OOB && h0 < p.half) {
-            const int64_t r = o >> 1;
-            *reinterpret_cast<uint32_t*>(p.aq + (r * p.a_blocks + block) * 16 + 8 * (kg & 1) + 4 * (kg >> 1)) = four;
-            if (kg == 0) p.as[(((int64_t)(block >> 4) * 4 + (block & 3)) * p.R + r) * 4 + ((block >> 2) & 3)] = (uint8_t)b;
+            top = max(top, is[j] ? t : 0u);
           }
+          const auto t16 = __builtin_amdgcn_permlane16_swap(top, top, false, false);
+          top = max(t16[0], t16[1]);
+          const auto t32 = __builtin_amdgcn_permlane32_swap(top, top, false, false);
+          top = max(t32[0], t32[1]);
+          const bool zero = o & 1u;
+          const int b = zero ? 0 : mx4_scale(top);
+          const uint32_t c0 = is[0] ? mx4_pack4(v[0], b) : 0u, c1 = is[1] ? mx4_pack4(v[1], b) : 0u;
+          // neighbouring lane groups make dwords: the even one of columns 0..15, the odd one of 16..31
+          const auto c = __builtin_amdgcn_permlane16_swap(c0, c1, false, false);
+          const bool stored = o != OOB && h0 < p.half;
+          const uint32_t r = o >> 1;
+          __builtin_amdgcn_raw_buffer_store_b32(zero ? 0u : c[0] | c[1] << 16, rQ, (int)(stored ? r * ((uint32_t)p.a_blocks * 16u) + q_at : OOB), 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b8((uint8_t)b, rS, (int)(stored && kg == 0 ? r * 4u + s_at : OOB), 0, 0);
         }
       });
     } else if (p.f32) {
