@@ -1,4 +1,4 @@
-"""Float64 checker of microscaled 4-bit floating point and of the products from it, written from their definitions; it shares no code with the
+"""Float64 oracle of microscaled 4-bit floating point and of the products from it, written from their definitions; it shares no code with the
 HIP path."""
 import numpy as np
 

@@ -7,8 +7,8 @@
 // the two bytes of its rows for a k tile, which the two steps of the tile select.
 // Tiles have two ring slots for either operand: the scales take the LDS of the third.
 //
-// Bound by power, and with short reductions by what stands outside the k loop: 8 experts of 4096 rows x 4096 x 14336, gated, 2110 us and 935 back (3.65 and
-// 4.12 PFLOP/s; the matrix pipes busy 54 % of the cycles at the 1.6 GHz that the power limit leaves): 1.7 to 1.85 us a k tile of 256 x 256 and 8 us a round
+// Bound by power, and with short reductions by what stands outside the k loop: 8 experts of 4096 rows x 4096 x 14336, gated, 2090 us and 960 back (3.68 and
+// 4.0 PFLOP/s; the matrix pipes busy 54 % of the cycles at the 1.6 GHz that the power limit leaves): 1.7 to 1.85 us a k tile of 256 x 256 and 8 us a round
 // of tiles, a chain of offsets, row map and first k tile (4 to 7, cold) and the epilogue (2 to 4).  64 experts of 512 rows x 2048 x 2048, 8 k tiles, 139 us (2.0 PFLOP/s).
 // Requests spread over less of the k tile, or over all of it, measured the same; four waves of 128 x 128, which read a third less
 // from LDS, with their accumulators in the other half of the register file 136 -> 144 us and 935 -> 1000; tiles of 64 x 128 were nowhere faster.

@@ -1,4 +1,4 @@
-"""The checker's microscaled 4-bit form of whole tensors at once, for the sizes at which its loops over blocks take too long; test_four_bits_cpu.py holds it
+"""The oracle's microscaled 4-bit form of whole tensors at once, for the sizes at which its loops over blocks take too long; test_four_bits_cpu.py holds it
 against them."""
 import numpy as np
 

@@ -1,11 +1,11 @@
-"""The vectorised 4-bit form of the tests is the checker's."""
+"""The vectorised 4-bit form of the tests is the oracle's."""
 import numpy as np
 
 import four_bits as F
 from oracle import mx4_oracle as O
 
 
-def test_it_is_the_checkers():
+def test_it_is_the_oracles():
     rng = np.random.default_rng(3)
     x = rng.standard_normal((60, 136)) * np.exp2(rng.integers(-130, 126, (60, 1)))
     x[::5] = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 0.0, -0.0, -0.25, -7.0, -5.0], (12, 136))

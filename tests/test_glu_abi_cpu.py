@@ -1,4 +1,4 @@
-"""Refusals of the gated FFN's entry points: everything is rejected on the host before a launch.  And the checker's gradients against
+"""Refusals of the gated FFN's entry points: everything is rejected on the host before a launch.  And the oracle's gradients against
 differences."""
 import ctypes
 
@@ -44,7 +44,7 @@ def test_glu_refusals():
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
-def test_checker_gradients_against_differences(act):
+def test_oracle_gradients_against_differences(act):
     rng = np.random.default_rng(2)
     offsets = np.array([0, 4, 4, 9])
     X, Wg, Wu = rng.standard_normal((11, 6)), rng.standard_normal((3, 6, 10)), rng.standard_normal((3, 6, 10))

@@ -1,5 +1,5 @@
 """GPU parity of the dropless block with gated experts: all of its calls strung together, against automatic differentiation in float64 with
-the block's own routing, served from 4 bits against the checker's, and replayed from a graph."""
+the block's own routing, served from 4 bits against the oracle's, and replayed from a graph."""
 import numpy as np
 import pytest
 import torch

@@ -1,4 +1,4 @@
-"""GPU parity of the gated expert FFN over ragged rows, forward, kept values and backward, against the float64 checker, element by element.
+"""GPU parity of the gated expert FFN over ragged rows, forward, kept values and backward, against the float64 oracle, element by element.
 
 Bounds.  Sums as in test_gpu_ragged.py: K 2^-23 of the sum of magnitudes in fp32.  bf16 stores round by 2^-8 of the value, fp32 stores by 2^-24.
 The bf16 GeLU is a polynomial off by 6e-5, its derivative by 1e-4; SiLU uses an exponential, a reciprocal and, in

@@ -1,4 +1,4 @@
-"""GPU parity of microscaled 4-bit floating point against the float64 checker: the bytes bit for bit, products and the gated FFN served from them
+"""GPU parity of microscaled 4-bit floating point against the float64 oracle: the bytes bit for bit, products and the gated FFN served from them
 element by element.
 
 Bounds.  Products of two 4-bit values are exact; a sum of K of them carries at most K 2^-23 of the sum of magnitudes in fp32, as in test_gpu_ragged.py.  Of

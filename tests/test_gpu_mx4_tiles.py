@@ -1,6 +1,6 @@
 """GPU parity of the products from 4 bits and of the gated FFN served from them in tiles of 256 x 256 (test_gpu_mx4.py has the kernel for few rows and
 tiles of 128 x 128): each size is one for which the dispatch chooses them, with k tiles that are full, cut short and a single one.  The tests, their
-checker and their bounds are those of test_gpu_mx4.py."""
+oracle and their bounds are those of test_gpu_mx4.py."""
 import pytest
 
 import test_gpu_mx4 as base

@@ -1,4 +1,4 @@
-"""Microscaled 4-bit floating point: pins of the checker, and what the entry points refuse before a launch."""
+"""Microscaled 4-bit floating point: pins of the oracle, and what the entry points refuse before a launch."""
 import ctypes
 
 import numpy as np
@@ -12,7 +12,7 @@ BIG = 1 << 60
 EINVAL, EUNSUPPORTED, EALIGN, EWORKSPACE, ENULL = -1, -2, -3, -5, -6
 
 
-def test_checker_scales_and_ties():
+def test_oracle_scales_and_ties():
     # the doubled scale starts where a / scale would round to 8, between 6 and 8
     for a, b in ((4.0, 127), (6.99, 127), (7.0, 128), (8.0, 128), (3.999, 127), (3.4, 126), (1.0, 125), (0.0, 0), (np.inf, 255), (1e-45, 0)):
         assert O.scale_byte(a) == b, a
@@ -22,7 +22,7 @@ def test_checker_scales_and_ties():
     assert list(O.code(O.SIZES, 127)) == list(range(8)) and O.code(np.array([-0.0]), 127)[0] == 8
 
 
-def test_checker_keeps_the_nearest():
+def test_oracle_keeps_the_nearest():
     rng = np.random.default_rng(1)
     x = rng.standard_normal((40, 100)) * np.exp2(rng.integers(-40, 40, (40, 1)))
     x[3] = 0
