@@ -127,15 +127,16 @@ struct Mx4 : Ragged {
       const uint32_t at = lds_b + tile_at(t);
       unrolled<0, NB>([&](auto j) { lds_read<decltype(j)::value * 64>(next_b[decltype(j)::value], at); });
     }
-    // B's, and row 0's of A, have landed.  Bytes of blocks that do not exist, which may be the byte of NaN, are taken as 2^-127: whatever the fragments
-    // hold there, the products with two of them are under 2^-240, zero in fp32.
+    // B's, and row 0's of A, have landed.  B's are moved by an instruction of its own behind the wait: as an assignment the compiler is free to copy them
+    // in front of it, and does (it takes them as written at the read).  Bytes of blocks that do not exist, which may be the byte of NaN, are taken as
+    // 2^-127: whatever the fragments hold there, the products with two of them are under 2^-240, zero in fp32.
     template <bool LAST>
     __device__ __forceinline__ void take_b(int t) {
       if constexpr (LAST) keep = (8 * t + q < blocks ? 0xFFu : 0u) | (8 * t + 4 + q < blocks ? 0xFF00u : 0u);
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        asm volatile("" : "+v"(next_b[j]));
-        b[j] = LAST ? next_b[j] & keep : next_b[j];
+        asm volatile("v_mov_b32 %0, %1" : "=v"(b[j]) : "v"(next_b[j]));
+        if constexpr (LAST) b[j] &= keep;
       }
     }
     template <bool LAST, int I>
