@@ -730,6 +730,7 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
   // The last tile (or, without k tiles, the prologue) has read a first step that nobody multiplies: its registers stay
   // taken until the reads have landed, or they would overwrite what the compiler puts there.
   frags_ready(0);
+  if constexpr (L::SCALED) sc.landed();
   __builtin_amdgcn_s_waitcnt(0x0070);  // every request is done before LDS is reused
   __syncthreads();
 

@@ -144,6 +144,13 @@ struct Mx4 : Ragged {
       asm volatile("" : "+v"(a[I]));
       if constexpr (LAST) a[I] &= keep;
     }
+    // Behind the last tile, whose reads for a next one nobody takes: every read has landed, and until then its register stayed taken.
+    __device__ __forceinline__ void landed() {
+#pragma unroll
+      for (int i = 0; i < MB; ++i) asm volatile("" : "+v"(a[i]));
+#pragma unroll
+      for (int j = 0; j < NB; ++j) asm volatile("" : "+v"(next_b[j]));
+    }
     template <int ST, int I, int J>
     __device__ __forceinline__ void product(f32x4_t& acc, const Frag& fb, const Frag& fa) {
       acc = mx4_mfma<ST>(make_uint4(fb.q[0], fb.q[1], fb.q[2], fb.q[3]), make_uint4(fa.q[0], fa.q[1], fa.q[2], fa.q[3]), acc, b[J], a[I]);
