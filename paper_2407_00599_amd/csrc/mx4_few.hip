@@ -126,6 +126,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
 #pragma unroll
     for (int q = 0; q < RG; ++q) {
       if (m0 + 16 * q >= n) break;                 // (uniform)
+      // rows of the group that have a token: of the others the products are zeros, also with weights that are not finite
+      const uint32_t real = (uint32_t)__ballot(x_off[q] != OOB);
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < NC; ++j)
@@ -143,6 +145,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
             t.y += a.y;
           }
           if (r >= n || col >= p.n) continue;
+          if (!(real >> row & 1u)) t = make_float2(0.f, 0.f);
           const int64_t at = (int64_t)(lo + r) * p.n + col;
           if (p.f32) *reinterpret_cast<float2*>(reinterpret_cast<float*>(p.C) + at) = t;
           else *reinterpret_cast<uint32_t*>(reinterpret_cast<bf16_t*>(p.C) + at) = pack_bf16x2(t.x, t.y);
@@ -162,7 +165,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
         uint32_t top = 0;
         with_hidden(p.act, p.f32, [&](auto act, auto wide) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) a[e] = hidden < p.half ? mx4_hidden<decltype(act)::value, decltype(wide)::value>(gv[e], uv[e]) : 0.f;
+          for (int e = 0; e < 8; ++e) a[e] = hidden < p.half && (real >> row & 1u) ? mx4_hidden<decltype(act)::value, decltype(wide)::value>(gv[e], uv[e]) : 0.f;
         });
 #pragma unroll
         for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(a[e]) & 0x7FFFFFFFu);

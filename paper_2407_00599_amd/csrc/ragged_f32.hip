@@ -41,10 +41,11 @@ struct Operand {       // one operand of a tile in LDS, and a thread's part in b
 template <int KIND, int T>
 constexpr int f32_floats() { return 2 * (Operand<T, KIND == KIND_TN>::FLOATS + Operand<T, KIND != KIND_NT>::FLOATS); }
 
-// Epilogues of the gated FFN.  Forward: 16 lanes hold g of a row and the 16 next to them its u.
+// Epilogues of the gated FFN.  Forward: 16 lanes hold g of a row and the 16 next to them its u; real: which of the tile's rows have a token, of the
+// others g and u are zeros, also with weights that are not finite.
 template <int EPI, int T, int ACT>
 __device__ __forceinline__ void store_glu(const RaggedArgs& p, const f32x16_t (&total)[T / 64][T / 64], const RaggedPlace& at, int m0, int n0,
-                                          int wm, int wn, int lane) {
+                                          int wm, int wn, int lane, const float* real) {
   constexpr int W = T / 2, NB = W / 32;
   const int l32 = lane & 31, half = lane >> 5;
   float* __restrict__ A = reinterpret_cast<float*>(p.C);      // act(g) u
@@ -55,9 +56,10 @@ __device__ __forceinline__ void store_glu(const RaggedArgs& p, const f32x16_t (&
     for (int r = 0; r < 16; ++r) {
       const int m = m0 + wm * W + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
       const int64_t row = at.lo + m;
+      const bool none = EPI != EPI_DGLU && real[m - m0] == 0.f;
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
-        const float v = total[i][j][r];
+        const float v = none ? 0.f : total[i][j][r];
         const int c = n0 + wn * W + 32 * j + l32;
         if constexpr (EPI == EPI_DGLU) {
           if (m >= at.n || c >= p.half) continue;
@@ -260,7 +262,13 @@ __device__ __forceinline__ void f32_tile(const RaggedArgs& p, float* smem, int v
   }
 
   if constexpr (GLU || EPI == EPI_DGLU) {
-    with_act(p.act, [&](auto act) { store_glu<EPI, T, decltype(act)::value>(p, total, at, m0, n0, wm, wn, lane); });
+    if constexpr (GLU) {
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < UA; ++u) smem[OA::at_of(tid, u)] = oka[u] ? 1.f : 0.f;      // (the threads of a row write the same)
+      __syncthreads();
+    }
+    with_act(p.act, [&](auto act) { store_glu<EPI, T, decltype(act)::value>(p, total, at, m0, n0, wm, wn, lane, smem); });
     return;
   }
   float* __restrict__ C = EPI == EPI_PART ? p.part : reinterpret_cast<float*>(p.C);

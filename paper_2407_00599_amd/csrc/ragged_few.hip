@@ -235,6 +235,8 @@ __device__ __forceinline__ void few_rows_glu(const FewArgs& p, float* red, int g
 #pragma unroll
   for (int q = 0; q < RG; ++q) {
     if (m0 + 16 * q >= n) break;                    // (uniform)
+    // rows of the group that have a token: of the others A is zeros, also with weights that are not finite
+    const uint32_t real = (uint32_t)__ballot(x_off[q] != OOB);
     float2 gs[UNITS], us[UNITS];
     auto meet = [&](const f32x4_t (&acc)[NCL], float2 (&sum)[UNITS]) {
       __syncthreads();
@@ -261,7 +263,8 @@ __device__ __forceinline__ void few_rows_glu(const FewArgs& p, float* red, int g
       constexpr int ACT = decltype(act)::value;
 #pragma unroll
       for (int v = 0; v < UNITS; ++v) {
-        const int at = tid + 64 * WAVES * v, row = m0 + 16 * q + at / (TH / 2), c = h0 + at % (TH / 2) * 2;
+        const int at = tid + 64 * WAVES * v, r = at / (TH / 2), row = m0 + 16 * q + r, c = h0 + at % (TH / 2) * 2;
+        if (!(real >> r & 1u)) gs[v] = us[v] = make_float2(0.f, 0.f);
         if (row < n && c < p.half)
           store_pair(p, lo + row, c, make_float2(gate_value<ACT, true>(gs[v].x) * us[v].x, gate_value<ACT, true>(gs[v].y) * us[v].y));
       }
