@@ -82,6 +82,7 @@ __device__ __forceinline__ uint32_t mx4_existing(const Mx4Args& p, uint32_t four
   return have >= 4 ? four : have <= 0 ? 0u : four & ((1u << (8 * have)) - 1u);
 }
 
+int mx4_tile(int64_t R, int E, int64_t n, int K);      // which of the kernels takes a product: 0 few rows, otherwise the tile
 void launch_mx4_few(Mx4Args a, int kind, hipStream_t st);
 void launch_mx4_tile(const Mx4Args& m, int kind, int tile, hipStream_t st);      // tiles of 256 x 256 or 128 x 128
 

@@ -23,19 +23,29 @@ void set_summed(Mx4Args& a, int K) {
 size_t tensor_bytes(int64_t n, int K) { return align_up(mx4_value_bytes(n, K), 256) + align_up(mx4_scale_bytes(n, K), 256); }
 
 // How a product is computed: 0, the kernel for few rows; 128 or 256, square tiles.  Experts of few rows are bound by their weights' bytes, which the kernel
-// for few rows reads fastest, but again for every 32 rows: 8 experts x 4096 x 14336 with 4, 16, 32 and 64 rows each 47, 59, 86 and 131 us, on
-// tiles of 128 58, 59, 61 and 64; 64 x 2048 x 2048 with 4, 16 and 32 28, 38 and 58, on tiles 33, 35 and 37.  Of the tiles the small ones waste less of
-// experts with few rows and fill the chip with fewer of them: rounds of tiles on the chip, each of k tiles of 256 and what is outside the k loop (us,
-// measured; with few and with all compute units busy).  8 x 4096 x 14336 with 64, 256, 1024 and 4096 rows each, tiles of 128 64, 124, 376 and
-// 1353 us, of 256 76, 111, 290 and 1092; 1 x 2048 x 8192 with 1024 and 4096 rows 18 and 55, 22 and 44.  Tiles of 64 x 128 were nowhere the fastest.
+// for few rows reads fastest, but again for every 16 rows of an expert (32 where more than 16 rows are of three experts or fewer), one reading after the
+// other in one workgroup.  How the rows are spread is not known here, so their number has a bound: up to 32 rows this is the faster one or nearly even
+// under any routing, beyond it it gains little with equal shares and loses the more if the experts' logits differ.  us of a product, this and tiles of 128, with equal
+// shares, logits that differ by N(0, 1) and by N(0, 2), and one expert with all rows:
+//    1 x 4096 x 14336   16 rows 9 and 16, 32 rows 10 and 16, 64 rows 18 and 18
+//    8 x 4096 x 14336   32 rows 49 and 55, 42 and 45, 41 and 49, 15 and 16;  64 rows 51 and 54, 70 and 53, 35 and 23, 26 and 18;
+//                      128 rows 56 and 55, 82 and 56, 67 and 52, 59 and 17
+//   64 x 2048 x 2048    16 rows 9 and 12, 10 and 10, 8 and 9, 8 and 9;  32 rows 15 and 16, 13 and 10, 10 and 10, 8 and 9;
+//                       64 rows 28 and 31, 15 and 14, 13 and 10, 14 and 9;  1024 rows 31 and 32, 55 and 24, 95 and 15, 132 and 10
+//  256 x 7168 x 2048    32 rows 49 and 52, 44 and 47, 27 and 30, 21 and 24;  64 rows 95 and 99, 69 and 54, 44 and 30, 38 and 24;
+//                      1024 rows 378 and 416, 267 and 147, 297 and 85, 557 and 30
+// Of the tiles the small ones waste less of experts with few rows and fill the chip with fewer of them: rounds of tiles on the chip, each of k tiles of
+// 256 and what is outside the k loop (us, measured; with few and with all compute units busy).  8 x 4096 x 14336 with 64, 256, 1024 and 4096 rows each, tiles of
+// 128 64, 124, 376 and 1353 us, of 256 76, 111, 290 and 1092; 1 x 2048 x 8192 with 1024 and 4096 rows 18 and 55, 22 and 44.  Tiles of 64 x 128 were nowhere the fastest.
 struct Mx4TileCost {
   int tile, per_cu;
   float k_few, k_all, fixed;
 };
 constexpr Mx4TileCost MX4_TILES[] = {{256, 1, 1.25f, 1.75f, 8.f}, {128, 2, 0.75f, 1.10f, 6.f}};
-constexpr int MX4_FEW_ROWS = 16;      // of an expert, on average
-int pick_tile(int64_t R, int E, int64_t n, int K) {
-  if (R <= (int64_t)MX4_FEW_ROWS * E) return 0;
+constexpr int MX4_FEW_ROWS = 32;
+}  // namespace
+int mx4_tile(int64_t R, int E, int64_t n, int K) {
+  if (R <= MX4_FEW_ROWS) return 0;
   const float nk = (float)((K + 255) / 256), cu = (float)num_cus();
   int best = 0;
   float best_t = 0.f;
@@ -49,8 +59,9 @@ int pick_tile(int64_t R, int E, int64_t n, int K) {
   }
   return best;
 }
+namespace {
 void launch(const Mx4Args& a, int kind, hipStream_t st) {
-  const int tile = pick_tile(a.R, a.E, a.n, a.K);
+  const int tile = mx4_tile(a.R, a.E, a.n, a.K);
   if (tile == 0) launch_mx4_few(a, kind, st);
   else launch_mx4_tile(a, kind, tile, st);
 }
