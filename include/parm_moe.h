@@ -365,10 +365,10 @@ int moe_ragged_ffn_bwd(const void* dY, const void* x, int dtype, int64_t S, cons
  *     dX = [dG | dU] W1^T,  dW1 = X^T [dG | dU],  dW2 = (act(g) u)^T dY
  *     dX [R, M];  dW1, dW2 FULL tensors, only the shard's columns / rows are written
  * A dense gated FFN is E = 1 with offsets {0, R} and inv = NULL.  Rows of Z and A behind offsets[E] are not
- * written, Y and dX hold zeros there.  Rows without a token have zeros in Z and A whatever W1 holds.  Z may be brought to 8 bits between the passes (moe_ckpt8_store).
- * fp32 accumulation, in fp32 from fp32 operands.  Workspace: backward, dG, dU, the recomputed activation and
- * parts of the weight gradients; forward, as moe_ragged_ffn_fwd.  Limits as there, with 2 H for H and
- * H <= 2^28. */
+ * written, Y and dX hold zeros there.  Rows without a token have zeros in Z and A whatever W1 holds.
+ * Z may be brought to 8 bits between the passes (moe_ckpt8_store).  fp32 accumulation, in fp32 from fp32
+ * operands.  Workspace: backward, dG, dU, the recomputed activation and parts of the weight gradients;
+ * forward, as moe_ragged_ffn_fwd.  Limits as there, with 2 H for H and H <= 2^28. */
 enum { MOE_ACT_SILU = 0, MOE_ACT_GELU = 1 };
 
 size_t moe_ragged_glu_workspace_bytes(int dtype, int64_t R, int E, int M, int H, int n_esp,
@@ -412,7 +412,9 @@ int moe_ckpt8_load(const void* q, const void* scales, int64_t rows, int cols, vo
  *   moe_mx4_store   x [G, rows, cols] -> G matrices; transposed = 0: n = rows, K = cols (activations);
  *                   transposed = 1: n = cols, K = rows (expert weights [E, K, N], which are summed over K)
  *   moe_mx4_load    back to x [G, rows, cols]
- * cols % 8 == 0, transposed also rows % 8 == 0.
+ * cols % 8 == 0, transposed also rows % 8 == 0.  A launch has fewer than 2^32 threads: pieces of 16 rows x 512
+ * columns (32 x 256 and 64 x 128 where a row has no more), transposed of 512 rows x 128 columns, are under 2^24
+ * (MOE_EUNSUPPORTED).
  *
  * moe_ragged_gemm_mx4: Y [R, N] = X W of each row's expert, rows and offsets as in moe_ragged_gemm;
  *   xq, xs  the token matrix (S rows of K; inv == NULL: R rows);  Wq, Ws  the experts' [E, K, N], stored with
@@ -420,10 +422,12 @@ int moe_ckpt8_load(const void* q, const void* scales, int64_t rows, int cols, vo
  *   Products are exact, sums fp32.
  * moe_ragged_glu_mx4: the gated FFN served from 4 bits.  x [S, M] (inv == NULL: [R, M]) of `dtype` is brought to
  *   4 bits row by row, G and U are its products with W1 [E, M, 2 H], A = act(G) U is brought to 4 bits row by row,
- *   Y [R, M] (dtype) = A W2, W2 [E, H, M]; both stored with transposed = 1.  Rows of A without a token are zeros.  A rank with a hidden shard stores
- *   its own columns / rows (H is then its share, Y a partial sum).  Workspace: x and A in 4 bits.
+ *   Y [R, M] (dtype) = A W2, W2 [E, H, M]; both stored with transposed = 1.  Rows of A without a token are
+ *   zeros.  A rank with a hidden shard stores its own columns / rows (H is then its share, Y a partial sum).
+ *   Workspace: x and A in 4 bits.
  * Limits: E <= 256, K, N, M, H multiples of 8, S*k and R at most 2^29, the 4-bit values of X, of A and of one
- * expert's matrix under 4 GiB each.
+ * expert's matrix under 4 GiB each; with n = N, or 2 H and M: min(E, R) * n under 2^30, E * n at most 2^34 and
+ * R * n at most 2^37 (MOE_EUNSUPPORTED).
  * --------------------------------------------------------------------------------------- */
 int moe_mx4_store(const void* x, int dtype, int64_t G, int64_t rows, int cols, int transposed, void* q,
                   void* scales, void* stream);

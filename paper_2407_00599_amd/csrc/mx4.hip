@@ -236,8 +236,10 @@ void with_lanes(int K, F&& f) {
   else if (K <= 256) f(std::integral_constant<int, 32>{});
   else f(std::integral_constant<int, 64>{});
 }
-int64_t grid_of(int64_t G, int64_t n, int K, int transposed) {      // the most workgroups that a call has
-  return G * mx4_chunks(K) * (transposed ? (n + COLS - 1) / COLS : (n + rows_of_group(64) - 1) / rows_of_group(64));
+double grid_of(int64_t G, int64_t n, int K, int transposed) {      // workgroups of a call (sizes that do not exist would overflow 64 bits)
+  int64_t groups = (n + COLS - 1) / COLS;
+  if (!transposed) with_lanes(K, [&](auto lanes) { groups = (n + rows_of_group(decltype(lanes)::value) - 1) / rows_of_group(decltype(lanes)::value); });
+  return (double)G * (double)mx4_chunks(K) * (double)groups;
 }
 
 template <typename T>
@@ -279,7 +281,8 @@ int check_mx4(int dtype, int64_t G, int64_t rows, int cols, int transposed) {
   MOE_REQUIRE(G >= 1 && rows >= 1 && cols >= 1 && (transposed == 0 || transposed == 1), MOE_EINVAL);
   MOE_REQUIRE(cols % 8 == 0 && (!transposed || rows % 8 == 0), MOE_EUNSUPPORTED);
   MOE_REQUIRE(G <= 1 << 20 && rows <= 1ll << 31 && (!transposed || rows < 1ll << 31), MOE_EUNSUPPORTED);
-  MOE_REQUIRE(transposed ? grid_of(G, cols, (int)rows, 1) < 1ll << 31 : grid_of(G, rows, cols, 0) < 1ll << 31, MOE_EUNSUPPORTED);
+  // a launch has fewer than 2^32 threads
+  MOE_REQUIRE((transposed ? grid_of(G, cols, (int)rows, 1) : grid_of(G, rows, cols, 0)) * MX4_THREADS < 4294967296.0, MOE_EUNSUPPORTED);
   return MOE_OK;
 }
 

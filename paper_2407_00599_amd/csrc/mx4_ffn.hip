@@ -43,9 +43,12 @@ struct Mx4TileCost {
 };
 constexpr Mx4TileCost MX4_TILES[] = {{256, 1, 1.25f, 1.75f, 8.f}, {128, 2, 0.75f, 1.10f, 6.f}};
 constexpr int MX4_FEW_ROWS = 32;
+// workgroups of `threads` threads each: a launch has fewer than 2^32 threads
+bool launches(int64_t groups, int threads) { return groups * threads < 1ll << 32; }
+int64_t few_groups(int E, int64_t n) { return E * ((n + 63) / 64) + ZERO_SHARES; }
 }  // namespace
 int mx4_tile(int64_t R, int E, int64_t n, int K) {
-  if (R <= MX4_FEW_ROWS) return 0;
+  if (R <= MX4_FEW_ROWS && launches(few_groups(E, n), 256)) return 0;
   const float nk = (float)((K + 255) / 256), cu = (float)num_cus();
   int best = 0;
   float best_t = 0.f;
@@ -72,7 +75,9 @@ int check_mx4_product(int64_t R, int E, int K, int64_t n) {
   MOE_REQUIRE(E <= MOE_MAX_E && K % 8 == 0 && n % 8 == 0, MOE_EUNSUPPORTED);
   MOE_REQUIRE(R <= 1ll << 29 && K <= 1 << 28 && n <= 1ll << 29, MOE_EUNSUPPORTED);
   MOE_REQUIRE(std::max(mx4_value_bytes(n, K), mx4_scale_bytes(n, K)) <= 0xFFFFFFF0ull, MOE_EUNSUPPORTED);
-  MOE_REQUIRE(R * n <= 1ll << 37 && (int64_t)E * n <= 1ll << 34, MOE_EUNSUPPORTED);     // tiles are counted in 32 bits
+  MOE_REQUIRE(R * n <= 1ll << 37 && (int64_t)E * n <= 1ll << 34, MOE_EUNSUPPORTED);
+  if (const int tile = mx4_tile(R, E, n, K))
+    MOE_REQUIRE(launches(most_row_tiles((int)R, E, tile) * ((n + tile - 1) / tile) + 8 + ZERO_SHARES, 2 * tile), MOE_EUNSUPPORTED);
   return MOE_OK;
 }
 int check_mx4_rows(int64_t rows, int K) {
