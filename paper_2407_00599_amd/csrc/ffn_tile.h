@@ -225,6 +225,8 @@ struct PlainOrder {
   template <int EPI>      // bytes that lie in front of k index row0 + at / 2 beside those of the k indexes before it
   static __device__ __forceinline__ uint32_t k_skip(const GemmArgs&, int, uint32_t) { return 0u; }
   static __device__ __forceinline__ int in_order(const GemmArgs&, int) { return 0; }     // added to entry `row` of a map
+  template <int KIND, int EPI, int MR, int NBK>      // bytes that store() uses of the wave's slice of LDS
+  static constexpr int staged_bytes() { return 32 * (64 * NBK + 16) * (EPI == EPI_GELU ? 2 : 1); }
   static constexpr bool SCALED = false;      // 4-bit operands with a scale for every 16 bytes of a row (mx4_tile.hip)
 };
 
@@ -314,7 +316,9 @@ __device__ __forceinline__ void gemm_dma_tile(const typename L::Args& p, char* s
   constexpr bool ONE = WK == 2 && MB < 2 && NB < 2;            // a single block: the second group's waves finish nothing
   const int e_i = (WK == 2 && MB >= 2) ? wk * EMB : 0, e_j = (WK == 2 && MB < 2 && NB >= 2) ? wk * ENB : 0;
   const int e_n = n0 + wn * WTN + 32 * e_j;
-  char* e_lds = smem + wave * (CF::LDS / CF::NW / 64 * 64);
+  constexpr int SLICE = CF::LDS / CF::NW / 64 * 64;            // of LDS, for a wave's epilogue
+  static_assert(EPI == EPI_PART || L::template staged_bytes<KIND, EPI, WK == 2 ? 32 : MR, ENB>() <= SLICE, "the epilogue's images");
+  char* e_lds = smem + wave * SLICE;
 
   // ---- k tiles: Kdim / 64 of a row-tiled GEMM, the walk over the expert's chunks for a weight gradient ----
   typename L::template Walk<EPI == EPI_PART && !PIECES> walk(p, at, part);

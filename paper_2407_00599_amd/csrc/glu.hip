@@ -35,6 +35,13 @@ struct Glu : Ragged {
   // Epilogues, staged through the wave's slice of LDS 32 rows at a time as in the other calls: images [32][CW] of up to three tensors, written in
   // accumulator order, read back row by row and stored 16 bytes a lane.  Of a piece of 32 tile columns a lane holds 4 (two times 4) values of the
   // gate and the up projection's of the same hidden columns.
+  static constexpr int pieces_of_step(int mr, int nbk) { return mr == 16 ? nbk : 1; }      // store_backward
+  template <int KIND, int EPI, int MR, int NBK>
+  static constexpr int staged_bytes() {
+    if (EPI == EPI_DGLU) return 3 * 32 * (64 * pieces_of_step(MR, NBK) + 16);
+    if (EPI == EPI_GLU || EPI == EPI_GLU_KEEP) return (EPI == EPI_GLU ? 1 : 3) * 32 * (32 * NBK + 16);
+    return Ragged::staged_bytes<KIND, EPI_STORE, MR, NBK>();
+  }
   template <int KIND, int EPI, int MR, int MB, int NBK, int AM, int AN>
   static __device__ __forceinline__ void store(const Args& p, typename AccBlock<MR>::type (&acc)[AM][AN], char* wave_lds, int g, int mwave,
                                                int mshift, int nbase, const uint32_t (&out_off)[2], int lane) {
@@ -114,7 +121,7 @@ struct Glu : Ragged {
   template <int ACT, int MR, int MB, int NBK, int AM, int AN>
   static __device__ __forceinline__ void store_backward(const Args& p, typename AccBlock<MR>::type (&acc)[AM][AN], char* wave_lds, int mshift,
                                                         int nbase, const uint32_t (&out_off)[2], int lane) {
-    constexpr int JB = MR == 16 ? NBK : 1, STEPS = MB * (NBK / JB);
+    constexpr int JB = pieces_of_step(MR, NBK), STEPS = MB * (NBK / JB);
     constexpr int CW = 32 * JB, PITCH = 2 * CW + 16, IMAGE = 32 * PITCH;
     constexpr int LPR = CW / 8, RPI = 64 / LPR, NT = 32 / RPI;
     constexpr int RG = 32 / MR, QG = 4 / RG;

@@ -82,6 +82,8 @@ struct Ragged : PlainOrder {
   // into [32][CW] images of the outputs, read back row by row and stored 16 bytes (8-bit values: 8 bytes) a lane.  The 32 columns of a
   // block of the 8-bit form are 32 columns of one wave's tile: their largest magnitude is 8 or 16 values of a lane and one or
   // two exchanges between lanes.
+  template <int KIND, int EPI, int MR, int NBK>
+  static constexpr int staged_bytes() { return 32 * (64 * NBK + 16) * (EPI == EPI_GELU8 || EPI == EPI_DGELU8 ? 2 : 1); }
   template <int KIND, int EPI, int MR, int MB, int NBK, int AM, int AN>
   static __device__ __forceinline__ void store(const Args& p, typename AccBlock<MR>::type (&acc)[AM][AN], char* wave_lds, int g,
                                                int mwave, int mshift, int nbase, const uint32_t (&out_off)[2], int lane) {
