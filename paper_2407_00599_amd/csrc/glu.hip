@@ -198,7 +198,6 @@ __global__ __launch_bounds__(64 * CF::NW) void glu_gemm_dma(const RaggedArgs p) 
 }
 
 using Tile256Brief = TileCfg<256, 256, 2, 4, 1, 3, 2, 32>;
-constexpr int BRIEF_ROWS = 4096;      // of an expert, on average
 
 // dX, dW2 and the gate's and the up projection's half of dW1, which only depend on dG, dU and A', in one launch; the last two read X's rows
 template <typename CFX, typename CFW, int EPI>
@@ -270,13 +269,13 @@ void launch_glu_backward(RaggedArgs dx, RaggedArgs w2, RaggedArgs wg, RaggedArgs
       if (w2.splits > 1) launch(Tile64x128{}, Tile128{}, std::integral_constant<int, EPI_PART>{});
       else launch(Tile64x128{}, Tile128{}, Store{});
     } else {
-      // A compute unit holds one workgroup of this launch whatever its tile (the LDS of a 256 x 256 one), so the tile of 192 rows gains nothing.  Weight
-      // gradients of few k tiles are not under the power limit and take 32 x 32 x 16 instructions.  dX in tiles of 192 and 256 rows, and those: 8 experts of 1024
-      // rows x 1024 x 4096 475, 437 and 432 us, 2 of 2048 x 2048 x 8192 728, 666 and 650; 1 of 32768 x 1024 x 2816 1414, 1347 and 1362.
+      // A compute unit holds one workgroup of this launch whatever its tile (the LDS of a 256 x 256 one), so the tile of 192 rows gains nothing: dX in tiles of
+      // 192 and of 256 rows, 8 experts of 1024 rows x 1024 x 4096 475 and 437 us, 2 of 2048 x 2048 x 8192 728 and 666.  The weight gradients take 32 x 32 x 16
+      // instructions; with 16 x 16 x 32 ones the call is within 2 % of it either way, us with these and with those: 8 experts x 1024 x 4096 of 1024, 4096, 8192
+      // and 16384 rows each 490 and 481, 1560 and 1555, 3005 and 3041, 6014 and 6010; 4 x 4096 x 7168 of 2048, 4096, 8192 and 16384 2437 and 2418, 4606 and
+      // 4624, 8957 and 9022, 17961 and 18053; 8 x 4096 x 7168 of 4096 9216 and 9307; 1 x 1024 x 2816 of 4096 and 32768 208 and 210, 1852 and 1858.
       const TilePlan t = plan_rows(dx, true);
-      const bool brief = dx.R <= BRIEF_ROWS * (int64_t)dx.G;
-      if (t.tile_m >= 192 && !brief) launch(Tile256{}, Tile256{}, Store{});
-      else if (t.tile_m >= 192) launch(Tile256{}, Tile256Brief{}, Store{});
+      if (t.tile_m >= 192) launch(Tile256{}, Tile256Brief{}, Store{});
       else if (t.tile_m == 128) launch(Tile128{}, Tile256Brief{}, Store{});
       else launch(Tile64x128{}, Tile256Brief{}, Store{});
     }
