@@ -2,7 +2,7 @@
 //
 // As in ragged_few.hip nothing is shared in the k loop: a lane's 16 bytes of a weight row are its operand of the scaled matrix instruction as they lie
 // in memory, and so are those of a row of X, from L2.  A wave takes units of 256 k, in which 16 rows give it whole 128-byte lines, for NC groups of 16
-// columns; the waves of a workgroup take the units in turn, some requested ahead, and their sums meet in LDS in a fixed order.  Of a gated first product
+// columns; the waves of a workgroup take the units in turn, the next one requested behind the products, and their sums meet in LDS in a fixed order.  Of a gated first product
 // the groups are the gate's and the up projection's of the same hidden columns in turn, and 32 hidden columns, one block of A, meet in one row of the
 // sums, so A goes to memory in 4 bits.
 //
@@ -11,11 +11,11 @@
 
 namespace moe {
 
-constexpr int MX4_NC = 4;      // groups of 16 columns
+constexpr int MX4_NC = 4, MX4_FEW_WAVES = 4;      // groups of 16 columns and waves of a workgroup
 
-template <int KIND, int RG, int WAVES, int PF>      // groups of 16 rows that go along with one reading of the weights; units requested ahead
-__global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
-  constexpr int NC = MX4_NC, TN = 16 * NC, PITCH = TN + 4;
+template <int KIND, int RG>      // groups of 16 rows that go along with one reading of the weights
+__global__ __launch_bounds__(64 * MX4_FEW_WAVES, 2) void mx4_few(const Mx4Args p) {
+  constexpr int NC = MX4_NC, WAVES = MX4_FEW_WAVES, TN = 16 * NC, PITCH = TN + 4;
   __shared__ float red[WAVES * 16 * PITCH];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c16 = lane & 15, kg = lane >> 4;
   const int tile = (int)blockIdx.x;
@@ -56,10 +56,10 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
       uint4 w[NC][2], x[RG][2];
       uint32_t ws[NC], xs[RG];
     };
-    Unit u[PF];
+    Unit d;
     // Offsets of this lane's rows are fixed, the unit's part of an address is in a scalar register.
     // No request and no product stands in a branch: their registers would be copied, and waited for, where the branches meet.
-    auto request_w = [&](Unit& d, int s) {         // blocks behind the last one: zeros
+    auto request_w = [&](int s) {         // blocks behind the last one: zeros
       const int at = min(s, units - 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -68,7 +68,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
 #pragma unroll
       for (int j = 0; j < NC; ++j) d.ws[j] = __builtin_amdgcn_raw_buffer_load_b32(rWS, (int)ws_off[j], (int)((uint32_t)at / 2u * 4u * w_scales), 0);
     };
-    auto request_x = [&](Unit& d, int s) {
+    auto request_x = [&](int s) {
       const int at = min(s, units - 1);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -82,11 +82,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
     for (int q = 0; q < RG; ++q)
 #pragma unroll
       for (int j = 0; j < NC; ++j) acc[q][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < PF; ++i) {
-      request_w(u[i], wave + WAVES * i);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    request_w(wave);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int q = 0; q < RG; ++q) {
       int row = m0 + 16 * q + c16 < n ? entry[q] : -1;
@@ -94,34 +91,26 @@ __global__ __launch_bounds__(64 * WAVES, 2) void mx4_few(const Mx4Args p) {
       x_off[q] = row >= 0 ? (uint32_t)row * pitch + (uint32_t)kg * 16u : OOB;
       xs_off[q] = row >= 0 ? (uint32_t)kg * x_scales + (uint32_t)row * 4u : OOB;
     }
+    request_x(wave);
+    __builtin_amdgcn_sched_barrier(0);
+    for (int s = wave; s < units; s += WAVES) {
+      const int c = s >> 1, sh = 16 * (s & 1);
+      uint32_t xs[RG];
 #pragma unroll
-    for (int i = 0; i < PF; ++i) {
-      request_x(u[i], wave + WAVES * i);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    for (int s0 = wave; s0 < units; s0 += WAVES * PF) {
+      for (int q = 0; q < RG; ++q) xs[q] = mx4_existing(p, d.xs[q], c, kg) >> sh;
 #pragma unroll
-      for (int i = 0; i < PF; ++i) {
-        const int s = s0 + WAVES * i;
-        Unit& d = u[i];
-        const int c = s >> 1, sh = 16 * (s & 1);
-        uint32_t xs[RG];
+      for (int j = 0; j < NC; ++j) {
+        const uint32_t ws = mx4_existing(p, d.ws[j], c, kg) >> sh;
 #pragma unroll
-        for (int q = 0; q < RG; ++q) xs[q] = mx4_existing(p, d.xs[q], c, kg) >> sh;
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          const uint32_t ws = mx4_existing(p, d.ws[j], c, kg) >> sh;
-#pragma unroll
-          for (int q = 0; q < RG; ++q) {
-            acc[q][j] = mx4_mfma<0>(d.x[q][0], d.w[j][0], acc[q][j], xs[q], ws);
-            acc[q][j] = mx4_mfma<1>(d.x[q][1], d.w[j][1], acc[q][j], xs[q], ws);
-          }
+        for (int q = 0; q < RG; ++q) {
+          acc[q][j] = mx4_mfma<0>(d.x[q][0], d.w[j][0], acc[q][j], xs[q], ws);
+          acc[q][j] = mx4_mfma<1>(d.x[q][1], d.w[j][1], acc[q][j], xs[q], ws);
         }
-        __builtin_amdgcn_sched_barrier(0);         // or the next unit's registers are taken before these are free
-        request_w(d, s + WAVES * PF);
-        request_x(d, s + WAVES * PF);
-        __builtin_amdgcn_sched_barrier(0);
       }
+      __builtin_amdgcn_sched_barrier(0);           // or the next unit's registers are taken before these are free
+      request_w(s + WAVES);
+      request_x(s + WAVES);
+      __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int q = 0; q < RG; ++q) {
@@ -185,19 +174,16 @@ static_assert(16 * MX4_NC / 2 == MX4_BLOCK, "a tile's hidden columns are one blo
 void launch_mx4_few(Mx4Args a, int kind, hipStream_t st) {
   a.tiles_n = kind == MX4_GLU ? (a.half + 8 * MX4_NC - 1) / (8 * MX4_NC) : (a.n + 16 * MX4_NC - 1) / (16 * MX4_NC);
   const dim3 grid((unsigned)(a.E * a.tiles_n + (kind == MX4_STORE ? ZERO_SHARES : 0)));
-  const bool one = a.R <= 8 * (int64_t)a.E || a.R <= 16;
-  auto launch = [&](auto k, auto rg, auto waves, auto pf) {
-    constexpr int W = decltype(waves)::value;
-    hipLaunchKernelGGL((mx4_few<decltype(k)::value, decltype(rg)::value, W, decltype(pf)::value>), grid, dim3(64 * W), 0, st, a);
+  auto launch = [&](auto k, auto rg) {
+    hipLaunchKernelGGL((mx4_few<decltype(k)::value, decltype(rg)::value>), grid, dim3(64 * MX4_FEW_WAVES), 0, st, a);
   };
   using std::integral_constant;
-  using W4 = integral_constant<int, 4>;
-  auto with_kind = [&](auto rg, auto pf) {
-    if (kind == MX4_GLU) launch(integral_constant<int, MX4_GLU>{}, rg, W4{}, pf);
-    else launch(integral_constant<int, MX4_STORE>{}, rg, W4{}, pf);
+  auto with_kind = [&](auto rg) {
+    if (kind == MX4_GLU) launch(integral_constant<int, MX4_GLU>{}, rg);
+    else launch(integral_constant<int, MX4_STORE>{}, rg);
   };
-  if (one) with_kind(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-  else with_kind(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+  if (a.R <= 8 * (int64_t)a.E || a.R <= 16) with_kind(integral_constant<int, 1>{});
+  else with_kind(integral_constant<int, 2>{});
 }
 
 }  // namespace moe
