@@ -309,28 +309,9 @@ inline void buffer_sizes(RaggedArgs& a, bool weights) {
   a.b_bytes = weights ? (uint64_t)a.R * (uint64_t)a.ldb * 2 : (uint64_t)a.G * (uint64_t)a.b_goff * 2;
 }
 
-// The tile of a bf16 row-tiled GEMM: the prices of the padded calls' tiles (ffn_tile.h) for what is multiplied, against the time of reading the
-// weights, 4.9 TB/s, priced as if a second row tile of an expert found half of them in a cache.  Weights bound the launch where experts have few rows, and a tile that
-// all rows of most experts fit in is then the fastest: 8 experts of 64 rows x 4096 x 14336 and x 14336 x 4096, tiles of 128 x 128 189 and 188 us,
-// 64 x 128 198 and 243, 64 x 64 227 and 249; of 1024 x 1024 x 4096 102 and 128, 192 x 256 82.
-// wide: only tiles of eight waves.
-inline TilePlan plan_rows(const RaggedArgs& a, bool wide = false) {
-  const float nk = (float)((a.Kdim + DK - 1) / DK), cu = (float)num_cus(), used = (float)std::min(a.R, a.G);
-  const float weights = used * (float)a.Kdim * (float)a.Ndim * 2.f / 4.9e6f;
-  TilePlan best{256, 256};
-  float best_t = 0.f;
-  for (const TileCost& c : ROW_TILES) {
-    if (wide && c.tile.tile_n == 64) continue;
-    const float row_tiles = (float)priced_row_tiles(a.R, a.G, c.tile.tile_m);
-    const float n = row_tiles * (float)((a.Ndim + c.tile.tile_n - 1) / c.tile.tile_n);
-    const float busy = c.per_cu == 1 ? n / cu : (n - cu) / cu;
-    const float k = c.k_few + (c.k_all - c.k_few) * fminf(fmaxf(busy, 0.f), 1.f);
-    const float products = ceilf(n / (cu * c.per_cu)) * (nk * k + c.fixed), reads = weights * 0.5f * (1.f + fmaxf(row_tiles / used, 1.f));
-    const float t = fmaxf(products, reads) + 0.2f * fminf(products, reads);
-    if (best_t == 0.f || t < best_t) { best_t = t; best = c.tile; }
-  }
-  return best;
-}
+// the tile of a bf16 row-tiled GEMM (ragged.hip); wide: only tiles of eight waves
+TilePlan rows_tile(int R, int E, int K, int N, bool wide);
+inline TilePlan plan_rows(const RaggedArgs& a, bool wide = false) { return rows_tile(a.R, a.G, a.Kdim, a.Ndim, wide); }
 
 // An fp32 product over rows with few tiles and a long reduction is cut into parts too, of at least ROW_PART_CHUNKS chunks of 32 k: 8 experts of
 // 256 rows x 2048 x 512 96 us whole, 68 in parts and 5 for adding them.
