@@ -419,7 +419,7 @@ int moe_ckpt8_load(const void* q, const void* scales, int64_t rows, int cols, vo
  * moe_ragged_gemm_mx4: Y [R, N] = X W of each row's expert, rows and offsets as in moe_ragged_gemm;
  *   xq, xs  the token matrix (S rows of K; inv == NULL: R rows);  Wq, Ws  the experts' [E, K, N], stored with
  *   transposed = 1;  Y of `dtype`, rows behind offsets[E] and rows without a token are zeros, whatever W holds.
- *   Products are exact, sums fp32.
+ *   Products are exact, sums fp32.  No workspace is needed: its size is 0, ws may be NULL.
  * moe_ragged_glu_mx4: the gated FFN served from 4 bits.  x [S, M] (inv == NULL: [R, M]) of `dtype` is brought to
  *   4 bits row by row, G and U are its products with W1 [E, M, 2 H], A = act(G) U is brought to 4 bits row by row,
  *   Y [R, M] (dtype) = A W2, W2 [E, H, M]; both stored with transposed = 1.  Rows of A without a token are

@@ -289,7 +289,10 @@ void launch_glu_backward(RaggedArgs dx, RaggedArgs w2, RaggedArgs wg, RaggedArgs
 // The kernels for few rows: as for the FFN with one projection, their number has a bound because an expert's weights are read again for every 16 of them.
 // Tiles and this, forward call: 2 rows, 8 experts x 1024 x 4096 26.4 and 19.9 us, 8 x 4096 x 14336 166 and 131; 64 rows 57.5 and 50.1, 567 and 509; but with
 // few weights the tiles' two launches are shorter, 2 rows of 64 x 2048 x 2048 24.0 and 24.6, 16 rows of 1 x 1024 x 2816 21.0 and 23.2, 32 rows of
-// 8 x 512 x 1536 18.9 and 19.3.
+// 8 x 512 x 1536 18.9 and 19.3.  With fewer hidden columns there is less to gain than to lose: tiles and this, equal shares, and one expert with all rows, 2 rows of
+// 16 x 7168 x 2048 74 and 76, 45 and 45, 32 rows 281 and 246, 50 and 128; 2 and 32 rows of 64 x 4096 x 1536 32 and 35, 31 and 33, 242 and 230, 35 and 95;
+// 32 rows of 64 x 2048 x 1024 89 and 81, 22 and 48, of 8 x 4096 x 4096 170 and 146, 42 and 90.  Within the rule the widest loss of this kind, 64 rows of
+// 8 x 1024 x 4096, is 57 and 48, 26 and 67.
 bool few_rows_glu(int dtype, int64_t R, int E, int M, int Hl) {
   return dtype == MOE_BF16 && (R <= 32 || (R <= 64 && R <= 8 * (int64_t)E)) && Hl >= 2 * (int64_t)M && std::min<int64_t>(R, E) * M * Hl >= 1 << 23;
 }

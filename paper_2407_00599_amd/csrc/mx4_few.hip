@@ -2,11 +2,12 @@
 //
 // As in ragged_few.hip nothing is shared in the k loop: a lane's 16 bytes of a weight row are its operand of the scaled matrix instruction as they lie
 // in memory, and so are those of a row of X, from L2.  A wave takes units of 256 k, in which 16 rows give it whole 128-byte lines, for NC groups of 16
-// columns; the waves of a workgroup take the units in turn, the next one requested behind the products, and their sums meet in LDS in a fixed order.  Of a gated first product
-// the groups are the gate's and the up projection's of the same hidden columns in turn, and 32 hidden columns, one block of A, meet in one row of the
-// sums, so A goes to memory in 4 bits.
+// columns; the waves of a workgroup take the units in turn, the next one requested behind the products, and their sums meet in LDS in a fixed order.
+// Of a gated first product the groups are the gate's and the up projection's of the same hidden columns in turn, and 32 hidden columns, one block
+// of A, meet in one row of the sums, so A goes to memory in 4 bits.
 //
-// Bound by HBM: 8 tokens top-2 of 8 experts x 4096 x 14336 84 us for the first product (499 MB of weights and scales, 5.9 TB/s) and 47 for the second (5.3).
+// Bound by HBM: 8 tokens top-2 of 8 experts x 4096 x 14336 83 to 85 us for the first product (499 MB of weights and scales, 5.9 TB/s) and 47 to 49
+// for the second (5.1 to 5.3).
 #include "mx4_ffn.h"
 
 namespace moe {

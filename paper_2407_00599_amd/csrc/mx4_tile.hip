@@ -36,7 +36,8 @@ struct Mx4 : Ragged {
     else return min(n0 + c, p.n - 1);
   }
   // Entry of the row map for row r of an expert (behind its last one: that one's).  Without a map nothing is read, and no branch stands
-  // around the read, so that all of a tile's are requested before the first is waited for (one after the other they took 2 us).
+  // around the read, so that those of a tile's operand and output rows are requested before the first is waited for (one after the other they took
+  // 2 us).  The entry of the row whose scales a lane brings (Scales) is one more read behind them.
   static __device__ __forceinline__ int entry(const Args& p, const Place& at, int r) {
     const __amdgpu_buffer_rsrc_t map = make_rsrc(p.gather, p.gather == nullptr ? 0u : (uint32_t)p.R * 4u);
     return (int)__builtin_amdgcn_raw_buffer_load_b32(map, (at.lo + min(r, at.n - 1)) * 4, 0, 0);
