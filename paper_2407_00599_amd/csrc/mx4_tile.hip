@@ -131,8 +131,11 @@ struct Mx4 : Ragged {
     // B's, and row 0's of A, have landed.  B's are moved by an instruction of its own behind the wait: as an assignment the compiler is free to copy them
     // in front of it, and does (it takes them as written at the read).  Bytes of blocks that do not exist, which may be the byte of NaN, are taken as
     // 2^-127: whatever the fragments hold there, the products with two of them are under 2^-240, zero in fp32.
+    // A product reads a register two instructions behind the vector instruction that wrote it at the earliest, and of an asm the compiler need not know that
+    // it is one: the first product reads b[0], NB - 1 moves behind its own.
     template <bool LAST>
     __device__ __forceinline__ void take_b(int t) {
+      static_assert(NB >= 3, "two wait states");
       if constexpr (LAST) keep = (8 * t + q < blocks ? 0xFFu : 0u) | (8 * t + 4 + q < blocks ? 0xFF00u : 0u);
 #pragma unroll
       for (int j = 0; j < NB; ++j) {
